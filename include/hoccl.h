@@ -504,6 +504,135 @@ hoccl_result_t hoccl_host_allreduce(const void* const* h_send, void* const* h_re
 hoccl_result_t hoccl_allreduce_static(const void* const* send, void* const* recv, size_t count, hoccl_dtype_t dtype,
                                       hoccl_op_t op, int R, hoccl_stream_t stream);
 
+/* ---------------------------------------------------------------- operators of a training step -- */
+
+/*
+ * (The paper has no counterpart: what a training step computes between its collectives, on the same buffers.)
+ *
+ * All of them: asynchronous kernel launches on `stream`, on the communicator's device, in stream order; the device that is current
+ * at the call stays current.  Nothing is allocated, so every call may be captured into a graph.  In handshake mode they are launched into
+ * the caller's stream like any other kernel.  They use the whole GPU ("sum_ctas" and "copy_ctas" do not bound them).  A call's results do
+ * not depend on what else runs; the same call on the same inputs gives the same bits.
+ * Calls with scratch use what hoccl_comm_set_scratch attached: calls that overlap in time on different streams need communicators of their own.
+ */
+
+/* How the averages of an AdamW step are kept: as binary32 numbers, or as e4m3 numbers (8 bits) with one binary32 scale for each block of
+ * HOCCL_STATE_BLOCK elements, counted from the tensor's (shard's) first element: value = code * scale, scale = largest |value| of the block / 448. */
+typedef enum { HOCCL_STATE_FLOAT32 = 0, HOCCL_STATE_8BIT = 1 } hoccl_state_t;
+#define HOCCL_STATE_BLOCK 256
+
+typedef struct {
+  void* param;             /* `count` weights, updated */
+  const void* grad;        /* their gradients, never written */
+  void* exp_avg;           /* m: count floats, or count bytes (HOCCL_STATE_8BIT) */
+  void* exp_avg_sq;        /* v: count floats; HOCCL_STATE_8BIT: count bytes that hold sqrt(v), which has half of v's range of exponents */
+  float* master;           /* NULL, or count binary32 weights that are updated and of which `param` (bf16) becomes the rounded copy */
+  float* exp_avg_scale;    /* HOCCL_STATE_8BIT: ceil(count / HOCCL_STATE_BLOCK) scales; else ignored */
+  float* exp_avg_sq_scale;
+  size_t count;            /* 0: the entry is ignored, its pointers may be NULL */
+  float weight_decay;
+} hoccl_adamw_tensor_t;
+
+/* What changes from step to step when the step is replayed from a graph: a 16-byte record in DEVICE memory (16-byte aligned). */
+typedef struct {
+  float lr, bias1, bias2;  /* bias1 = 1 - beta1^step, bias2 = 1 - beta2^step */
+  uint32_t seed;
+} hoccl_adamw_rates_t;
+
+typedef struct {
+  double lr, beta1, beta2, eps;  /* finite; 0 <= beta < 1; eps > 0 */
+  double grad_scale;             /* the gradients are multiplied by it (1 / R for a mean over R ranks) */
+  long step;                     /* 1 for the first */
+  uint32_t seed;                 /* HOCCL_STATE_8BIT: of the rounding; another one each step */
+  const float* factor;           /* DEVICE float or NULL: multiplies the gradients too (hoccl_grad_norm's out + 1); NaN: the step leaves everything as it is */
+  const hoccl_adamw_rates_t* rates;  /* DEVICE record or NULL: takes the place of lr, step and seed */
+} hoccl_adamw_config_t;
+
+/*
+ * AdamW step over many tensors.  A plan holds the table of tensors; it is made once (host only, no device needed) and used for as many steps
+ * as its buffers live.  For element i of a tensor, in binary32 (s = grad_scale * factor, t = step):
+ *     g = s * grad;  m = beta1 * m + (1 - beta1) * g;  v = beta2 * v + (1 - beta2) * g^2
+ *     p = p * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * with p = master, or param where there is none (a bf16 param without a master is rounded at every step, to nearest even).
+ * The weights are computed from m and v as they are before they are stored.  HOCCL_STATE_8BIT stores m and sqrt(v) with stochastic rounding:
+ * u = value * (448 / largest of the block) becomes the e4m3 number below or above it, above with the probability of its distance from the one
+ * below in units of 1/65536, so that an average that moves by less than a step of e4m3 (6 to 12 %) still moves; sqrt(v) > 0 never
+ * becomes 0.  The random bits of element i (h = its tensor's number in the table, mix = the 32-bit finalizer of MurmurHash3):
+ * w = mix(lo(i) + hi(i) * 632BE5AB + mix(seed + h * 9E3779B9)); m takes w mod 2^16, sqrt(v) takes w >> 16.  A block whose largest value is at most 1e-35
+ * is stored as zeros.  A gradient that is not finite makes its element's weights and states NaN or infinite (8-bit states: of its block); a `factor` from hoccl_grad_norm
+ * skips such a step.
+ * Any alignment of a tensor to its element size is served; tensors whose arrays all start on 16-byte boundaries are faster.  Tensors and arrays must not
+ * overlap, gradients excepted among themselves.  Either every tensor has a master or none; param_dtype must then be HOCCL_BFLOAT16.
+ * hoccl_adamw_create errors: INVALID_ARG (NULL, n < 0, misaligned, overlapping, masters of some tensors only, weight_decay not finite),
+ * UNSUPPORTED (dtype, state, a master beside fp32 weights), INTERNAL (out of host memory).
+ * hoccl_adamw_step errors: INVALID_ARG (NULL, a number out of its range, misaligned factor or rates), CUDA.  A plan is only read by a step.
+ */
+typedef struct hoccl_adamw_plan* hoccl_adamw_plan_t;
+hoccl_result_t hoccl_adamw_create(hoccl_adamw_plan_t* plan, const hoccl_adamw_tensor_t* tensors, int n, hoccl_dtype_t param_dtype,
+                                  hoccl_dtype_t grad_dtype, hoccl_state_t state);
+void hoccl_adamw_destroy(hoccl_adamw_plan_t plan);
+hoccl_result_t hoccl_adamw_step(hoccl_adamw_plan_t plan, const hoccl_adamw_config_t* config, hoccl_comm_t comm, hoccl_stream_t stream);
+
+/*
+ * Sharded AdamW step: reduce-scatter of the gradients, AdamW on every rank's shard, all-gather of the weights, as one kernel.
+ * grads[r], params[r]: rank r's `count` gradients and weights.  Rank c keeps the state of ring chunk c = elements [c q, min((c+1) q, count)),
+ * q = ceil(count / R) as in hoccl_allreduce: exp_avg[c], exp_avg_sq[c], master[c], exp_avg_scale[c] and exp_avg_sq_scale[c] hold that chunk from its
+ * first element on (blocks of 8-bit states too; c is the tensor's number h).  The gradient of chunk c is grad_scale * factor * (((x_{c+1} + x_{c+2}) + ...) + x_c):
+ * the ring's order of adds, in binary32 and, unlike hoccl_reduce_scatter, never rounded to the gradients' dtype in between.  The new weights go to every
+ * params[r]; without masters they are computed from params[c].  The step with a clipped norm, which needs the summed gradient first, is hoccl_reduce_scatter,
+ * hoccl_grad_norm, hoccl_adamw_step on the shards, hoccl_allgather.  No scratch.
+ * master: NULL or R pointers; the scales may be NULL with HOCCL_STATE_FLOAT32.  Pointers of an empty chunk may be NULL.  No two arrays may overlap.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA as hoccl_adamw_create and hoccl_adamw_step.
+ */
+hoccl_result_t hoccl_sharded_adamw(const void* const* grads, void* const* params, void* const* exp_avg, void* const* exp_avg_sq, float* const* master,
+                                   float* const* exp_avg_scale, float* const* exp_avg_sq_scale, size_t count, hoccl_dtype_t param_dtype,
+                                   hoccl_dtype_t grad_dtype, hoccl_state_t state, float weight_decay, const hoccl_adamw_config_t* config,
+                                   hoccl_comm_t comm, hoccl_stream_t stream);
+
+/*
+ * Norm of the n vectors grads[k] (counts[k] elements each) as one vector: out[0] = sqrt(sum of squares), summed in binary64, and
+ * out[1] = min(1, max_norm / (out[0] + 1e-6)), the factor that clips to max_norm; NaN if a gradient is not finite.  out: two DEVICE floats.
+ * max_norm > 0, infinity for no clipping.  Needs hoccl_grad_norm_scratch_bytes() of scratch.  Empty vectors may be NULL; no vectors: 0 and 1.
+ * Errors: INVALID_ARG (NULL, misaligned, max_norm), UNSUPPORTED (dtype), SCRATCH, CUDA.
+ */
+size_t hoccl_grad_norm_scratch_bytes(void);
+hoccl_result_t hoccl_grad_norm(const void* const* grads, const size_t* counts, int n, hoccl_dtype_t dtype, double max_norm, float* out,
+                               hoccl_comm_t comm, hoccl_stream_t stream);
+
+/*
+ * Router of an expert-parallel layer.  Rank r has tokens[r] rows of `experts` logits (dtype; `ld` elements from row to row, ld >= experts) and gets, row by row,
+ *   indices[r][k], k < topk: the experts of the topk largest logits, largest first, of equal ones the lowest index first; -1 where fewer than topk
+ *                  logits are above -infinity (a masked expert; a row with none is padding: it chooses nothing and counts nowhere);
+ *   weights[r][k]: their probabilities p = softmax(row), divided by their sum if `normalize`; 0 beside -1;
+ * and counts[r], experts + 1 ints: how often each expert was chosen, then the number of rows that chose any: what the counts of an hoccl_alltoallv are made of.
+ * loss (two floats for each group) and saved (experts + 1 floats for each group): over the n such rows of all ranks (one group), or of each rank by itself
+ * (`per_rank`: R groups), with f_e = count of e / (topk * n) and P_e = the rows' sum of p_e / n:
+ *   loss[0] = balance_coef * experts * sum of f_e P_e;  loss[1] = z_coef * (the rows' sum of log(sum of exp(logits))^2) / n; both 0 if n is 0;
+ *   saved = balance_coef * experts * f_e / n for each expert, then 2 * z_coef / n: what hoccl_route_backward needs.
+ * A NaN logit is never chosen; it makes its row's weights and the losses NaN, as +infinity does.  counts, f and P are exact or summed in a fixed order.
+ *
+ * hoccl_route_backward: dlogits[r] (rows of `dld` elements) = dloss[group] * d(loss[0] + loss[1])/dlogits, f held fixed, + the gradient that dweights[r] (tokens[r] x topk)
+ * gives through the weights; with `logits`, `indices`, `saved`, the shape and the flags of the forward call.  dloss: DEVICE floats, one for each group, NULL for ones;
+ * dweights: NULL for none.  Entries of dweights beside an index outside 0 .. experts-1 are ignored; rows without an open expert get zeros.
+ * dlogits[r] may be logits[r] with dld == ld; what lies between the rows is left as it is.
+ *
+ * indices, weights, dweights, counts: contiguous.  1 <= topk <= min(32, experts), experts <= 1024, tokens[r] < 2^31 (0: that rank's pointers may be NULL, but counts[r] is written).
+ * Forward needs hoccl_route_scratch_bytes of scratch.  Outputs must not overlap each other or an input (but as stated).
+ * Errors: INVALID_ARG (NULL, misaligned, a number out of its range, a region of outputs that overlaps another region), UNSUPPORTED (dtype), SCRATCH, CUDA.
+ */
+typedef struct {
+  int experts, topk;
+  hoccl_dtype_t dtype;     /* of the logits and their gradients */
+  int normalize, per_rank; /* 0 or 1 */
+  double balance_coef, z_coef;   /* finite; not used by the backward call */
+} hoccl_route_config_t;
+size_t hoccl_route_scratch_bytes(int R, size_t max_tokens, int experts);
+hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* tokens, const hoccl_route_config_t* config, int32_t* const* indices,
+                           float* const* weights, int32_t* const* counts, float* loss, float* saved, hoccl_comm_t comm, hoccl_stream_t stream);
+hoccl_result_t hoccl_route_backward(const void* const* logits, size_t ld, const size_t* tokens, const hoccl_route_config_t* config,
+                                    const int32_t* const* indices, const float* saved, const float* const* dweights, const float* dloss,
+                                    void* const* dlogits, size_t dld, hoccl_comm_t comm, hoccl_stream_t stream);
+
 /* ---------------------------------------------------------------- errors and statistics -------- */
 
 const char* hoccl_error_string(hoccl_result_t code);

@@ -20,6 +20,8 @@ SUM = 0
 PATH_CE, PATH_SM, PATH_CE_HOST = 0, 1, 2
 
 DTYPES = {"fp32": FLOAT32, "bf16": BFLOAT16}
+STATES = {"fp32": 0, "8bit": 1}   # how the averages of an AdamW step are kept
+STATE_BLOCK = 256                 # elements that share a scale in 8-bit states
 
 EXPORTS = [   # every function include/hoccl.h declares
     "hoccl_comm_init", "hoccl_comm_destroy", "hoccl_scratch_bytes", "hoccl_scratch_bytes_direct",
@@ -30,7 +32,8 @@ EXPORTS = [   # every function include/hoccl.h declares
     "hoccl_profile_reset", "hoccl_allreduce_static", "hoccl_sched_build", "hoccl_sched_destroy",
     "hoccl_sched_num_stages", "hoccl_sched_stage_tau", "hoccl_sched_total_tau", "hoccl_sched_lower_bound",
     "hoccl_sched_matrix", "hoccl_sched_num_flows", "hoccl_sched_get_flow", "hoccl_sched_queue_len",
-    "hoccl_sched_queue_get",
+    "hoccl_sched_queue_get", "hoccl_adamw_create", "hoccl_adamw_destroy", "hoccl_adamw_step", "hoccl_sharded_adamw",
+    "hoccl_grad_norm_scratch_bytes", "hoccl_grad_norm", "hoccl_route_scratch_bytes", "hoccl_route", "hoccl_route_backward",
 ]
 
 
@@ -51,6 +54,12 @@ class Stats(ctypes.Structure):
 class SchedFlow(ctypes.Structure):
     _fields_ = [("src", ctypes.c_int), ("dst", ctypes.c_int), ("cls", ctypes.c_int), ("origin_src", ctypes.c_int),
                 ("origin_dst", ctypes.c_int), ("bytes", ctypes.c_uint64), ("origin_offset", ctypes.c_uint64)]
+
+
+class AdamTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
+                ("master", ctypes.c_void_p), ("exp_avg_scale", ctypes.c_void_p), ("exp_avg_sq_scale", ctypes.c_void_p),
+                ("count", ctypes.c_size_t), ("weight_decay", ctypes.c_float)]
 
 
 FLOW_NATIVE, FLOW_RDMA, FLOW_FWD_SEND, FLOW_FWD_RECV = 0, 1, 2, 3
@@ -114,6 +123,10 @@ def lib() -> ctypes.CDLL:
         "hoccl_comm_proxy_stats": (i, [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), i]),
         "hoccl_host_allreduce": (i, [vpp, vpp, sz, i, i, vp, vp]),
         "hoccl_allreduce_static": (i, [vpp, vpp, sz, i, i, i, vp]),
+        "hoccl_adamw_create": (i, [vpp, ctypes.POINTER(AdamTensor), i, i, i, i]),
+        "hoccl_adamw_destroy": (None, [vp]),
+        "hoccl_grad_norm_scratch_bytes": (sz, []),
+        "hoccl_route_scratch_bytes": (sz, [i, sz, i]),
         "hoccl_error_string": (ctypes.c_char_p, [i]),
         "hoccl_last_cuda_error": (ctypes.c_char_p, [vp]),
         "hoccl_last_stats": (i, [vp, ctypes.POINTER(Stats)]),
@@ -131,7 +144,8 @@ def lib() -> ctypes.CDLL:
 
 
 # functions called through csrc/calls.c, in the order its bind() takes them
-_INNER_LOOP = ["allreduce", "reduce_scatter", "host_allreduce", "allgather", "alltoall", "alltoallv", "send", "recv", "allreduce_static"]
+_INNER_LOOP = ["allreduce", "reduce_scatter", "host_allreduce", "allgather", "alltoall", "alltoallv", "send", "recv", "allreduce_static",
+               "adamw_step", "sharded_adamw", "grad_norm", "route", "route_backward"]
 
 
 def error_string(code: int) -> str:
@@ -167,6 +181,83 @@ def _dtype(d) -> int:
     if isinstance(d, str):
         return DTYPES[d]
     return int(d)
+
+
+def _state(s) -> int:
+    return STATES[s] if isinstance(s, str) else int(s)
+
+
+def _count_of(x, k: int, counts) -> int:
+    if counts is not None:
+        return int(counts[k])
+    if not x.is_contiguous():
+        raise ValueError("tensor %d is not contiguous" % k)
+    return int(x.numel())
+
+
+class Tensors:
+    """A list of vectors marshalled once (grad_norm): their addresses, their lengths (of contiguous tensors, or `counts`) and dtype."""
+
+    def __init__(self, xs: Sequence, dtype, counts: Optional[Sequence[int]] = None):
+        self.n, self.dtype, self._keep = len(xs), _dtype(dtype), list(xs)
+        self._ptrs = _ptr_array(xs)
+        self._counts = (ctypes.c_size_t * self.n)(*[_count_of(x, k, counts) for k, x in enumerate(xs)])
+        self._at = ctypes.addressof(self._ptrs), ctypes.addressof(self._counts)
+
+
+class AdamTensors:
+    """The table of one hoccl_adamw_plan_t: lists of as many tensors (or addresses, with `counts`) as there are weights.
+
+    state "fp32" or "8bit" (then with scales); weight_decay: one number, or one for each tensor.  The tensors are kept alive."""
+
+    def __init__(self, params: Sequence, grads: Sequence, exp_avg: Sequence, exp_avg_sq: Sequence, param_dtype, grad_dtype, state="fp32", master=None,
+                 exp_avg_scale=None, exp_avg_sq_scale=None, weight_decay=0.0, counts: Optional[Sequence[int]] = None):
+        self._h = ctypes.c_void_p()
+        n = len(params)
+        lists = {"param": params, "grad": grads, "exp_avg": exp_avg, "exp_avg_sq": exp_avg_sq, "master": master, "exp_avg_scale": exp_avg_scale,
+                 "exp_avg_sq_scale": exp_avg_sq_scale}
+        table = (AdamTensor * max(n, 1))()
+        for k in range(n):
+            table[k].count = _count_of(params[k], k, counts)
+            table[k].weight_decay = float(weight_decay[k]) if hasattr(weight_decay, "__getitem__") else float(weight_decay)
+        blocks = [(table[k].count + STATE_BLOCK - 1) // STATE_BLOCK for k in range(n)]
+        for name, xs in lists.items():
+            if xs is None:
+                continue
+            if len(xs) != n:
+                raise ValueError("%d %s tensors, %d wanted" % (len(xs), name, n))
+            for k, x in enumerate(xs):
+                if hasattr(x, "is_contiguous"):
+                    want = blocks[k] if name.endswith("_scale") else table[k].count
+                    if not x.is_contiguous() or x.numel() < want:
+                        raise ValueError("%s[%d]: %d contiguous elements are wanted" % (name, k, want))
+                setattr(table[k], name, _ptr(x))
+        rc = lib().hoccl_adamw_create(ctypes.byref(self._h), table, n, _dtype(param_dtype), _dtype(grad_dtype), _state(state))
+        if rc != OK:
+            raise HocclError(rc, "hoccl_adamw_create")
+        self._keep = {name: list(xs) for name, xs in lists.items() if xs is not None}
+
+    def destroy(self):
+        if self._h:
+            lib().hoccl_adamw_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def adamw_rates(lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, seed: int = 0):
+    """The record that a captured AdamW step reads (hoccl_adamw_rates_t) as a CPU tensor of four 32-bit words, to be copied to the device between replays."""
+    import math
+    import struct
+
+    import torch
+
+    bias = [-math.expm1(step * math.log(b)) if b else 1.0 for b in (beta1, beta2)]
+    return torch.frombuffer(bytearray(struct.pack("<fffI", lr, *bias, seed & 0xFFFFFFFF)), dtype=torch.int32)
 
 
 class Comm:
@@ -269,6 +360,31 @@ class Comm:
     def host_allreduce(self, h_send, h_recv, count, dtype, stream=None, op=SUM):
         self._check(_calls.host_allreduce(self._h.value, h_send, h_recv, count, dtype, op, stream), "hoccl_host_allreduce")
 
+    # -- operators of a training step
+    def adamw(self, tensors: AdamTensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, factor=None, rates=None, seed=0, stream=None):
+        """hoccl_adamw_step.  factor: device float (grad_norm's out[1:]); rates: device record (adamw_rates) in place of lr, step and seed."""
+        self._check(_calls.adamw_step(self._h.value, tensors._h.value, lr, step, beta1, beta2, eps, grad_scale, factor, rates, seed, stream), "hoccl_adamw_step")
+
+    def sharded_adamw(self, grads, params, exp_avg, exp_avg_sq, count, param_dtype, grad_dtype, lr, step, state="fp32", master=None, exp_avg_scale=None,
+                      exp_avg_sq_scale=None, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, grad_scale=1.0, factor=None, rates=None, seed=0, stream=None):
+        self._check(_calls.sharded_adamw(self._h.value, grads, params, exp_avg, exp_avg_sq, master, exp_avg_scale, exp_avg_sq_scale, count, param_dtype, grad_dtype,
+                                         _state(state), weight_decay, lr, step, beta1, beta2, eps, grad_scale, factor, rates, seed, stream), "hoccl_sharded_adamw")
+
+    def grad_norm(self, grads: Tensors, out, max_norm=float("inf"), stream=None):
+        """out: two device floats, the norm and the factor that clips to max_norm."""
+        self._check(_calls.grad_norm(self._h.value, grads._at[0], grads._at[1], grads.n, grads.dtype, max_norm, out, stream), "hoccl_grad_norm")
+
+    def route(self, logits, tokens, experts, topk, dtype, indices, weights, counts, loss, saved, balance_coef=0.01, z_coef=0.0, normalize=True, per_rank=False,
+              ld=None, stream=None):
+        """ld: elements from one row of the logits to the next (None: experts)."""
+        self._check(_calls.route(self._h.value, logits, experts if ld is None else ld, tokens, experts, topk, dtype, normalize, per_rank, balance_coef, z_coef, indices,
+                                 weights, counts, loss, saved, stream), "hoccl_route")
+
+    def route_backward(self, logits, tokens, experts, topk, dtype, indices, saved, dweights, dloss, dlogits, normalize=True, per_rank=False, ld=None, dld=None,
+                       stream=None):
+        self._check(_calls.route_backward(self._h.value, logits, experts if ld is None else ld, tokens, experts, topk, dtype, normalize, per_rank, indices, saved, dweights,
+                                          dloss, dlogits, experts if dld is None else dld, stream), "hoccl_route_backward")
+
     # -- point to point
     def send_rc(self, buf, count, dtype, src, dst, stream=None) -> int:
         return _calls.send(self._h.value, buf, count, dtype, src, dst, stream)
@@ -323,6 +439,14 @@ def scratch_bytes(R: int, max_count: int, dtype) -> int:
 def scratch_bytes_direct(R: int, max_count: int, dtype) -> int:
     """Scratch bound with "rs_direct" set (R-1 inbox slots per rank)."""
     return int(lib().hoccl_scratch_bytes_direct(R, max_count, _dtype(dtype)))
+
+
+def grad_norm_scratch_bytes() -> int:
+    return int(lib().hoccl_grad_norm_scratch_bytes())
+
+
+def route_scratch_bytes(R: int, max_tokens: int, experts: int) -> int:
+    return int(lib().hoccl_route_scratch_bytes(R, max_tokens, experts))
 
 
 class Schedule:

@@ -14,6 +14,8 @@
 #include <stdint.h>
 #include <string.h>
 
+#include "../../include/hoccl.h"
+
 #define MAX_RANKS 64
 
 typedef int (*coll_op_fn)(const void* const*, void* const*, size_t, int, int, void*, void*);
@@ -22,7 +24,7 @@ typedef int (*static_fn)(const void* const*, void* const*, size_t, int, int, int
 typedef int (*pattern_fn)(const void* const*, const size_t*, const size_t*, void* const*, const size_t*, int, void*, void*);
 typedef int (*p2p_fn)(void*, size_t, int, int, int, void*, void*);
 
-enum { F_ALLREDUCE, F_REDUCE_SCATTER, F_HOST_ALLREDUCE, F_ALLGATHER, F_ALLTOALL, F_ALLTOALLV, F_SEND, F_RECV, F_STATIC, F_COUNT };
+enum { F_ALLREDUCE, F_REDUCE_SCATTER, F_HOST_ALLREDUCE, F_ALLGATHER, F_ALLTOALL, F_ALLTOALLV, F_SEND, F_RECV, F_STATIC, F_ADAMW, F_SHARDED, F_NORM, F_ROUTE, F_ROUTE_BACKWARD, F_COUNT };
 static void* g_fn[F_COUNT];
 static PyObject *g_data_ptr, *g_cuda_stream;          /* interned attribute names */
 static PyObject *g_current_device, *g_current_stream; /* torch's: () -> device index, (device index) -> raw stream */
@@ -242,6 +244,126 @@ static PyObject* py_alltoallv(PyObject* m, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(rc);
 }
 
+static int as_double(PyObject* o, double* out) {
+  *out = PyFloat_AsDouble(o);
+  return *out == -1.0 && PyErr_Occurred() ? -1 : 0;
+}
+
+/* lr, step, beta1, beta2, eps, grad_scale, factor, rates, seed */
+#define ADAMW_ARGS 9
+static int as_adamw_config(PyObject* const* a, hoccl_adamw_config_t* c) {
+  void *factor, *rates;
+  size_t step, seed;
+  if (as_double(a[0], &c->lr) || as_size(a[1], &step) || as_double(a[2], &c->beta1) || as_double(a[3], &c->beta2) || as_double(a[4], &c->eps) ||
+      as_double(a[5], &c->grad_scale) || as_address(a[6], &factor) || as_address(a[7], &rates) || as_size(a[8], &seed))
+    return -1;
+  c->step = (long)step;
+  c->seed = (uint32_t)seed;
+  c->factor = factor;
+  c->rates = rates;
+  return 0;
+}
+
+/* (comm, plan, the step's numbers, stream) */
+static PyObject* py_adamw_step(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  void *comm, *plan, *stream;
+  hoccl_adamw_config_t c;
+  int rc;
+  if (n_args(n, 3 + ADAMW_ARGS) || as_address(a[0], &comm) || as_address(a[1], &plan) || as_adamw_config(a + 2, &c) || as_stream(a[2 + ADAMW_ARGS], &stream)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((hoccl_result_t(*)(hoccl_adamw_plan_t, const hoccl_adamw_config_t*, hoccl_comm_t, hoccl_stream_t))g_fn[F_ADAMW])(plan, &c, comm, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* A sequence of buffers or None: the pointer to pass on. */
+static int as_addresses_or_null(PyObject* o, void** room, void*** out) {
+  *out = o == Py_None ? NULL : room;
+  return o == Py_None ? 0 : as_addresses(o, room);
+}
+
+/* (comm, grads, params, exp_avg, exp_avg_sq, master, exp_avg_scale, exp_avg_sq_scale, count, param_dtype, grad_dtype, state, weight_decay, the step's numbers, stream) */
+static PyObject* py_sharded_adamw(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  void *comm, *stream, *room[7][MAX_RANKS], **p[7];
+  size_t count;
+  int pd, gd, state, rc;
+  double decay;
+  hoccl_adamw_config_t c;
+  if (n_args(n, 14 + ADAMW_ARGS) || as_address(a[0], &comm)) return NULL;
+  for (int k = 0; k < 7; k++)
+    if (as_addresses_or_null(a[1 + k], room[k], &p[k])) return NULL;
+  if (as_size(a[8], &count) || as_dtype(a[9], &pd) || as_dtype(a[10], &gd) || as_int(a[11], &state) || as_double(a[12], &decay) || as_adamw_config(a + 13, &c) ||
+      as_stream(a[13 + ADAMW_ARGS], &stream))
+    return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((hoccl_result_t(*)(const void* const*, void* const*, void* const*, void* const*, float* const*, float* const*, float* const*, size_t, hoccl_dtype_t, hoccl_dtype_t,
+                           hoccl_state_t, float, const hoccl_adamw_config_t*, hoccl_comm_t, hoccl_stream_t))g_fn[F_SHARDED])(
+      (const void* const*)p[0], p[1], p[2], p[3], (float* const*)p[4], (float* const*)p[5], (float* const*)p[6], count, (hoccl_dtype_t)pd, (hoccl_dtype_t)gd,
+      (hoccl_state_t)state, (float)decay, &c, comm, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* (comm, address of the table of pointers, of the counts, n, dtype, max_norm, out, stream) */
+static PyObject* py_grad_norm(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  void *comm, *grads, *counts, *out, *stream;
+  int k, dtype, rc;
+  double max_norm;
+  if (n_args(n, 8) || as_address(a[0], &comm) || as_address(a[1], &grads) || as_address(a[2], &counts) || as_int(a[3], &k) || as_dtype(a[4], &dtype) ||
+      as_double(a[5], &max_norm) || as_address(a[6], &out) || as_stream(a[7], &stream))
+    return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((hoccl_result_t(*)(const void* const*, const size_t*, int, hoccl_dtype_t, double, float*, hoccl_comm_t, hoccl_stream_t))g_fn[F_NORM])(grads, counts, k, (hoccl_dtype_t)dtype,
+                                                                                                                      max_norm, out, comm, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* experts, topk, dtype, normalize, per_rank */
+static int as_route_config(PyObject* const* a, hoccl_route_config_t* c) {
+  int dtype;
+  if (as_int(a[0], &c->experts) || as_int(a[1], &c->topk) || as_dtype(a[2], &dtype) || as_int(a[3], &c->normalize) || as_int(a[4], &c->per_rank)) return -1;
+  c->dtype = (hoccl_dtype_t)dtype;
+  c->balance_coef = c->z_coef = 0;
+  return 0;
+}
+
+/* (comm, logits, ld, tokens, [5 of the shape], balance_coef, z_coef, indices, weights, counts, loss, saved, stream) */
+static PyObject* py_route(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  void *comm, *stream, *loss, *saved, *logits[MAX_RANKS], *indices[MAX_RANKS], *weights[MAX_RANKS], *counts[MAX_RANKS];
+  size_t ld, tokens[MAX_RANKS] = {0};
+  int rc;
+  hoccl_route_config_t c;
+  if (n_args(n, 17) || as_address(a[0], &comm) || as_addresses(a[1], logits) || as_size(a[2], &ld) || as_sizes(a[3], MAX_RANKS, tokens) ||
+      as_route_config(a + 4, &c) || as_double(a[9], &c.balance_coef) || as_double(a[10], &c.z_coef) || as_addresses(a[11], indices) || as_addresses(a[12], weights) ||
+      as_addresses(a[13], counts) || as_address(a[14], &loss) || as_address(a[15], &saved) || as_stream(a[16], &stream))
+    return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((hoccl_result_t(*)(const void* const*, size_t, const size_t*, const hoccl_route_config_t*, int32_t* const*, float* const*, int32_t* const*, float*, float*, hoccl_comm_t,
+                           hoccl_stream_t))g_fn[F_ROUTE])((const void* const*)logits, ld, tokens, &c, (int32_t* const*)indices, (float* const*)weights, (int32_t* const*)counts, loss,
+                                                          saved, comm, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* (comm, logits, ld, tokens, [5 of the shape], indices or None, saved, dweights or None, dloss, dlogits, dld, stream) */
+static PyObject* py_route_backward(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  void *comm, *stream, *saved, *dloss, *logits[MAX_RANKS], *indices[MAX_RANKS], *dweights[MAX_RANKS], *dlogits[MAX_RANKS], **ip, **dp;
+  size_t ld, dld, tokens[MAX_RANKS] = {0};
+  int rc;
+  hoccl_route_config_t c;
+  if (n_args(n, 16) || as_address(a[0], &comm) || as_addresses(a[1], logits) || as_size(a[2], &ld) || as_sizes(a[3], MAX_RANKS, tokens) ||
+      as_route_config(a + 4, &c) || as_addresses_or_null(a[9], indices, &ip) || as_address(a[10], &saved) || as_addresses_or_null(a[11], dweights, &dp) ||
+      as_address(a[12], &dloss) || as_addresses(a[13], dlogits) || as_size(a[14], &dld) || as_stream(a[15], &stream))
+    return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = ((hoccl_result_t(*)(const void* const*, size_t, const size_t*, const hoccl_route_config_t*, const int32_t* const*, const float*, const float* const*, const float*, void* const*,
+                           size_t, hoccl_comm_t, hoccl_stream_t))g_fn[F_ROUTE_BACKWARD])((const void* const*)logits, ld, tokens, &c, (const int32_t* const*)ip, saved,
+                                                                                         (const float* const*)dp, dloss, dlogits, dld, comm, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 /* The addresses of the library's functions, in the order of the enumeration above. */
 static PyObject* py_bind(PyObject* m, PyObject* const* a, Py_ssize_t n) {
   if (n_args(n, F_COUNT)) return NULL;
@@ -253,7 +375,8 @@ static PyObject* py_bind(PyObject* m, PyObject* const* a, Py_ssize_t n) {
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {ENTRY(bind),     ENTRY(allreduce), ENTRY(reduce_scatter), ENTRY(host_allreduce),
                                 ENTRY(allgather), ENTRY(alltoall),  ENTRY(alltoallv),      ENTRY(send),
-                                ENTRY(recv),      ENTRY(allreduce_static), {NULL, NULL, 0, NULL}};
+                                ENTRY(recv),      ENTRY(allreduce_static), ENTRY(adamw_step), ENTRY(sharded_adamw),
+                                ENTRY(grad_norm), ENTRY(route),     ENTRY(route_backward), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__calls(void) {

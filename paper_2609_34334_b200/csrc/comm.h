@@ -190,6 +190,20 @@ inline bool ranges_overlap(const char* a, size_t an, const char* b, size_t bn) {
   return a < b + bn && b < a + an;
 }
 
+// Makes the communicator's device current for one call and the device that was current so again behind it.
+struct DeviceScope {
+  int before = -1;
+  cudaError_t err;
+  explicit DeviceScope(int device) {
+    err = cudaGetDevice(&before);
+    if (err == cudaSuccess && before == device) before = -1;
+    else if (err == cudaSuccess) err = cudaSetDevice(device);
+  }
+  ~DeviceScope() {
+    if (before >= 0) cudaSetDevice(before);
+  }
+};
+
 struct Call {
   int kind;  // PlanKind
   size_t count;

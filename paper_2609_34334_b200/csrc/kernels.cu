@@ -1014,6 +1014,11 @@ bool add_chain_seg(ChainBatch* b, const void* const* ops, int nops, void* const*
 }
 
 cudaError_t launch_in_order(const void* fn, int grid, int threads, void* args, cudaStream_t stream, int priority) {
+  void* params[1] = {args};
+  return launch_in_order_params(fn, grid, threads, params, stream, priority);
+}
+
+cudaError_t launch_in_order_params(const void* fn, int grid, int threads, void** params, cudaStream_t stream, int priority, size_t smem) {
   cudaStreamCaptureStatus capture;
   const cudaError_t e = cudaStreamIsCapturing(stream, &capture);
   if (e != cudaSuccess) return e;
@@ -1021,6 +1026,7 @@ cudaError_t launch_in_order(const void* fn, int grid, int threads, void* args, c
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cfg.attrs = attr;
   if (capture == cudaStreamCaptureStatusNone) {
@@ -1031,7 +1037,6 @@ cudaError_t launch_in_order(const void* fn, int grid, int threads, void* args, c
     attr[cfg.numAttrs].id = cudaLaunchAttributePriority;
     attr[cfg.numAttrs++].val.priority = priority;
   }
-  void* params[1] = {args};
   return cudaLaunchKernelExC(&cfg, fn, params);
 }
 
@@ -1282,6 +1287,8 @@ static std::vector<const void*> dispatched_kernels() {
     for (int form = 0; form < 4; form++) fns.push_back(store_all_of(R, form & 1, form & 2));
   for (int shape = 0; shape < (int)(sizeof(kMoveShapes) / sizeof(kMoveShapes[0])); shape++)
     for (const void* f : {move_entry<MoveBatch>(shape), move_entry<MoveBatchSmall>(shape)}) fns.push_back(f);
+  add_optim_kernels(&fns);
+  add_router_kernels(&fns);
   std::sort(fns.begin(), fns.end());
   fns.erase(std::unique(fns.begin(), fns.end()), fns.end());
   return fns;

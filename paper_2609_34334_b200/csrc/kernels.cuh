@@ -3,6 +3,7 @@
 #pragma once
 #include <cuda_runtime.h>
 #include <cstdint>
+#include <vector>
 
 namespace hoccl {
 
@@ -213,6 +214,10 @@ void prepare_ring_phase(RingSeg* seg, int nseg, int kind, int dtype, int threads
 // (wait_for_stream), so the order and what a kernel sees are those of a plain launch.  `fn` must be such a kernel.
 // Without the attribute while the stream is being captured: the capture keeps full edges.
 cudaError_t launch_in_order(const void* fn, int grid, int threads, void* args, cudaStream_t stream, int priority = 0);
+cudaError_t launch_in_order_params(const void* fn, int grid, int threads, void** params, cudaStream_t stream, int priority = 0, size_t smem = 0);   // several parameters
+// The kernels that the operators of a training step may launch (optim.cu, router.cu).
+void add_optim_kernels(std::vector<const void*>* fns);
+void add_router_kernels(std::vector<const void*>* fns);
 
 // Enqueue helpers (return the CUDA error of the launch).
 cudaError_t launch_sum(const SumBatch& batch, int ctas, cudaStream_t stream);

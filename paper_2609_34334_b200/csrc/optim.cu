@@ -1,0 +1,813 @@
+// The operators of a training step that read gradients: the AdamW step over many tensors, the same step on R ranks with sharded
+// state (reduce-scatter, update, all-gather in one kernel) and the gradient norm.  (The paper has no counterpart.)
+//
+// All three stream: HBM bounds them.  An element of a bf16 weight with a binary32 master and states moves 28 bytes (gradient 2, master, m
+// and v 4 in and 4 out, weight 2 out) and takes some 20 instructions; with 8-bit states 16 bytes and some 70.
+// The unit of work is a block of 256 elements, one warp's: the elements that share a scale in 8-bit states, so that a block's
+// largest value is one warp reduction and states of either kind have one shape.  In an aligned, whole block lane l holds elements 8 l .. 8 l + 7 (32-byte
+// accesses of binary32 arrays, 16 of bf16, 8 of codes); in any other one elements l, l + 32, ...  Both run the same arithmetic: alignment changes no bit.
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "comm.h"
+#include "device_common.cuh"
+
+using namespace hoccl;
+
+namespace hoccl {
+namespace {
+
+constexpr int kBlock = HOCCL_STATE_BLOCK;
+constexpr int kWarps = 8, kOptThreads = 32 * kWarps;
+static_assert(kBlock == 256, "a warp holds a block with 8 elements a lane");
+
+// weights: binary32; bf16; bf16 beside a binary32 master
+enum { W_FP32 = 0, W_BF16 = 1, W_MASTER = 2 };
+
+struct AdamScalars {
+  float lr, step_size, root_scale;   // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  float beta1, grad1, beta2, grad2;  // grad1 = 1 - beta1, grad2 = 1 - beta2, rounded once
+  float eps, grad_scale;
+  unsigned seed;
+  const float* factor;
+  const hoccl_adamw_rates_t* rates;
+};
+
+struct AdamRow {
+  void *param, *m, *v;
+  const void* grad;
+  float *master, *m_scale, *v_scale;
+  unsigned long long n;
+  float decay;
+  unsigned flags;   // bit 0: aligned; the rest: number of the tensor in the caller's table
+};
+// Tensors by value: a launch carries up to 32 (2.4 KB of parameters) or up to 420 (32 KB, the most there is).
+template <int N>
+struct AdamTableT {
+  unsigned blocks, per_warp;    // blocks of all tensors; of one warp
+  int n, pad;
+  AdamRow row[N];
+  unsigned first[N + 1];        // prefix sums of blocks
+};
+using AdamTableSmall = AdamTableT<32>;
+using AdamTable = AdamTableT<420>;
+static_assert(sizeof(AdamTable) + sizeof(AdamScalars) <= 32764, "kernel parameters");
+
+struct ShardedArgs {
+  int R;
+  float decay;
+  unsigned per_rank, per_warp;   // blocks of a full chunk; of one warp
+  unsigned long long count, q;
+  unsigned long long aligned;    // bit c: chunk c
+  const void* grad[kMaxRanks];
+  void* param[kMaxRanks];
+  void *m[kMaxRanks], *v[kMaxRanks];
+  float *master[kMaxRanks], *m_scale[kMaxRanks], *v_scale[kMaxRanks];
+};
+
+// ---------------------------------------------------------------- device: memory
+
+// Eight consecutive elements of an aligned array, read or written once: no reuse to keep lines for.
+__device__ __forceinline__ void load8(const float* p, float* x) {
+  asm volatile("ld.global.L1::no_allocate.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+               : "l"(p)
+               : "memory");
+}
+__device__ __forceinline__ void store8(float* p, const float* x) {
+  asm volatile("st.global.L1::no_allocate.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]),
+               "f"(x[5]), "f"(x[6]), "f"(x[7])
+               : "memory");
+}
+__device__ __forceinline__ void widen8(uint4 r, float* x) {
+  const unsigned w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
+  unsigned d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
+// Where a lane's eight elements lie in its block, and which of them exist.
+template <bool VEC>
+__device__ __forceinline__ unsigned element(int lane, int i) {
+  return VEC ? lane * 8 + i : i * 32 + lane;
+}
+
+// DT 0 binary32, 1 bf16.  `left`: elements of the array from the block's start (VEC: at least 256).
+template <int DT, bool VEC>
+__device__ __forceinline__ void load_floats(const void* base, unsigned long long at, unsigned left, int lane, float* x) {
+  if (DT == 0) {
+    const float* p = static_cast<const float*>(base) + at;
+    if (VEC) {
+      load8(p + lane * 8, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) x[i] = i * 32 + lane < left ? __ldcs(p + i * 32 + lane) : 0.0f;
+    }
+  } else {
+    const unsigned short* p = static_cast<const unsigned short*>(base) + at;
+    if (VEC) {
+      widen8(__ldcs(reinterpret_cast<const uint4*>(p) + lane), x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) x[i] = i * 32 + lane < left ? __uint_as_float((unsigned)__ldcs(p + i * 32 + lane) << 16) : 0.0f;
+    }
+  }
+}
+template <int DT, bool VEC>
+__device__ __forceinline__ void store_floats(void* base, unsigned long long at, unsigned left, int lane, const float* x) {
+  if (DT == 0) {
+    float* p = static_cast<float*>(base) + at;
+    if (VEC) {
+      store8(p + lane * 8, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        if (i * 32 + lane < left) __stcs(p + i * 32 + lane, x[i]);
+    }
+  } else {
+    unsigned short* p = static_cast<unsigned short*>(base) + at;
+    if (VEC) {
+      __stcs(reinterpret_cast<uint4*>(p) + lane, make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        if (i * 32 + lane < left) __stcs(p + i * 32 + lane, __bfloat16_as_ushort(__float2bfloat16_rn(x[i])));
+    }
+  }
+}
+
+// ---------------------------------------------------------------- device: 8-bit states
+
+// The 32-bit finalizer of MurmurHash3 (Appleby, public domain).
+__device__ __forceinline__ unsigned mix(unsigned h) {
+  h = (h ^ (h >> 16)) * 0x85EBCA6Bu;
+  h = (h ^ (h >> 13)) * 0xC2B2AE35u;
+  return h ^ (h >> 16);
+}
+__device__ __forceinline__ unsigned tensor_key(unsigned seed, unsigned tensor) { return mix(seed + tensor * 0x9E3779B9u); }
+__device__ __forceinline__ unsigned element_word(unsigned key, unsigned long long i) { return mix((unsigned)i + (unsigned)(i >> 32) * 0x632BE5ABu + key); }
+
+template <bool VEC>
+__device__ __forceinline__ void load_codes(const void* base, unsigned long long at, unsigned left, int lane, float scale, float* x) {
+  const unsigned char* p = static_cast<const unsigned char*>(base) + at;
+  unsigned short pair[4];
+  if (VEC) {
+    const uint2 r = __ldcs(reinterpret_cast<const uint2*>(p) + lane);
+    pair[0] = (unsigned short)r.x;
+    pair[1] = (unsigned short)(r.x >> 16);
+    pair[2] = (unsigned short)r.y;
+    pair[3] = (unsigned short)(r.y >> 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const unsigned lo = 2 * i * 32 + lane < left ? __ldcs(p + 2 * i * 32 + lane) : 0, hi = (2 * i + 1) * 32 + lane < left ? __ldcs(p + (2 * i + 1) * 32 + lane) : 0;
+      pair[i] = (unsigned short)(lo | hi << 8);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(pair[i], __NV_E4M3)));
+    x[2 * i] = f.x * scale;
+    x[2 * i + 1] = f.y * scale;
+  }
+}
+
+// One number on the grid of e4m3 (3 bits of mantissa from 2^-6 on, steps of 2^-9 below), rounded down or, with the chance of what is
+// cut off, up.  Adding 2^-6 to a number below 2^-6 puts it where binary32's own grid of 3 bits has those steps.  `rnd`: 16 random bits.
+__device__ __forceinline__ float round_e4m3(float u, unsigned rnd) {
+  const float a = fabsf(u), shift = a < 0.015625f ? 0.015625f : 0.0f;
+  const unsigned b = (__float_as_uint(a + shift) + (rnd << 4)) & 0xfff00000u;
+  return copysignf(__uint_as_float(b) - shift, u);
+}
+
+// Stores a block (x >= 0 for the root) and its scale.  The whole warp takes part.
+template <bool VEC, bool ROOT>
+__device__ __forceinline__ void store_codes(void* base, float* scales, unsigned long long at, unsigned left, int lane, const float* x, const unsigned* word) {
+  unsigned top_bits = 0;
+#pragma unroll
+  for (int i = 0; i < 8; i++) top_bits = max(top_bits, __float_as_uint(x[i]) & 0x7fffffffu);   // NaN is the largest
+  const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, top_bits));
+  const bool some = top > 1e-35f;
+  const float inv = some ? 448.0f / top : 0.0f;
+  if (lane == 0) scales[at / kBlock] = some ? top * (1.0f / 448.0f) : top == top ? 0.0f : top;
+  unsigned short pair[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    float q[2];
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+      const float u = x[2 * i + j] * inv;
+      q[j] = round_e4m3(u, ROOT ? word[2 * i + j] >> 16 : word[2 * i + j] & 0xffffu);
+      if (ROOT && u > 0.0f) q[j] = fmaxf(q[j], 0.001953125f);
+    }
+    pair[i] = __nv_cvt_float2_to_fp8x2(make_float2(q[0], q[1]), __NV_SATFINITE, __NV_E4M3);
+  }
+  unsigned char* p = static_cast<unsigned char*>(base) + at;
+  if (VEC) {
+    __stcs(reinterpret_cast<uint2*>(p) + lane, make_uint2(pair[0] | (unsigned)pair[1] << 16, pair[2] | (unsigned)pair[3] << 16));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+      if (i * 32 + lane < left) p[i * 32 + lane] = (unsigned char)(pair[i / 2] >> (i % 2 * 8));
+  }
+}
+
+// ---------------------------------------------------------------- device: the step
+
+struct Rates {
+  float lr, step_size, root_scale, scale;
+  unsigned seed;
+  bool skip;
+};
+__device__ __forceinline__ Rates read_rates(const AdamScalars& s) {
+  Rates r{s.lr, s.step_size, s.root_scale, s.grad_scale, s.seed, false};
+  if (s.rates) {
+    const uint4 x = *reinterpret_cast<const uint4*>(s.rates);
+    r.lr = __uint_as_float(x.x);
+    r.step_size = r.lr / __uint_as_float(x.y);
+    r.root_scale = 1.0f / sqrtf(__uint_as_float(x.z));
+    r.seed = x.w;
+  }
+  if (s.factor) {
+    const float f = *s.factor;
+    r.skip = f != f;
+    r.scale *= f;
+  }
+  return r;
+}
+
+__device__ __forceinline__ float sqrt_fast(float x) {   // off by at most 2^-23 of the root
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// What a block's state and weight need besides its gradient.
+template <int W, int STATE, bool VEC>
+struct Held {
+  float p[8], m[8], v[8];
+  // weights: W_MASTER from the master, else from param
+  __device__ __forceinline__ void load(const void* param, const float* master, const void* mp, const void* vp, const float* ms, const float* vs,
+                                       unsigned long long weight_at, unsigned long long at, unsigned left, int lane) {
+    if (W == W_MASTER) load_floats<0, VEC>(master, at, left, lane, p);
+    else load_floats<W == W_FP32 ? 0 : 1, VEC>(param, weight_at, left, lane, p);
+    if (STATE == HOCCL_STATE_FLOAT32) {
+      load_floats<0, VEC>(mp, at, left, lane, m);
+      load_floats<0, VEC>(vp, at, left, lane, v);
+    } else {
+      load_codes<VEC>(mp, at, left, lane, ms[at / kBlock], m);
+      load_codes<VEC>(vp, at, left, lane, vs[at / kBlock], v);
+    }
+  }
+  // g: the gradients as they were read.  Afterwards p holds the new weights, which the caller stores; the state is stored here.
+  __device__ __forceinline__ void step(const float* g, const AdamScalars& s, const Rates& r, float keep, unsigned key, float* master, void* mp, void* vp,
+                                       float* ms, float* vs, unsigned long long at, unsigned left, int lane) {
+    float root[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const float x = g[i] * r.scale;
+      m[i] = s.beta1 * m[i] + s.grad1 * x;
+      v[i] = s.beta2 * (STATE == HOCCL_STATE_8BIT ? v[i] * v[i] : v[i]) + s.grad2 * (x * x);
+      root[i] = sqrt_fast(v[i]);
+      p[i] = p[i] * keep - r.step_size * __fdividef(m[i], root[i] * r.root_scale + s.eps);
+    }
+    if (W == W_MASTER) store_floats<0, VEC>(master, at, left, lane, p);
+    if (STATE == HOCCL_STATE_FLOAT32) {
+      store_floats<0, VEC>(mp, at, left, lane, m);
+      store_floats<0, VEC>(vp, at, left, lane, v);
+    } else {
+      unsigned word[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++) word[i] = element_word(key, at + element<VEC>(lane, i));
+      store_codes<VEC, false>(mp, ms, at, left, lane, m, word);
+      store_codes<VEC, true>(vp, vs, at, left, lane, root, word);
+    }
+  }
+};
+
+template <int GT, int W, int STATE, bool VEC>
+__device__ __forceinline__ void tensor_block(const AdamRow& t, const AdamScalars& s, const Rates& r, unsigned block, int lane) {
+  const unsigned long long at = (unsigned long long)block * kBlock;
+  const unsigned left = (unsigned)min(t.n - at, (unsigned long long)kBlock);
+  Held<W, STATE, VEC> h;
+  float g[8];
+  load_floats<GT, VEC>(t.grad, at, left, lane, g);
+  h.load(t.param, t.master, t.m, t.v, t.m_scale, t.v_scale, at, at, left, lane);
+  h.step(g, s, r, fmaf(-r.lr, t.decay, 1.0f), STATE == HOCCL_STATE_8BIT ? tensor_key(r.seed, t.flags >> 1) : 0, t.master, t.m, t.v, t.m_scale, t.v_scale, at,
+         left, lane);
+  store_floats<W == W_FP32 ? 0 : 1, VEC>(t.param, at, left, lane, h.p);
+}
+
+template <int GT, int W, int STATE, class Table>
+__global__ void __launch_bounds__(kOptThreads) adamw_kernel(const __grid_constant__ Table t, const __grid_constant__ AdamScalars s) {
+  wait_for_stream();
+  const Rates r = read_rates(s);
+  if (r.skip) return;
+  const int lane = threadIdx.x & 31;
+  const unsigned b0 = (blockIdx.x * kWarps + threadIdx.x / 32) * t.per_warp;
+  if (b0 >= t.blocks) return;
+  const unsigned b1 = min(b0 + t.per_warp, t.blocks);
+  int k = 0;
+  for (int step = t.n <= 32 ? 16 : 256; step; step >>= 1)   // the last tensor that starts at or before b0
+    if (k + step < t.n && t.first[k + step] <= b0) k += step;
+  for (unsigned b = b0; b < b1; b++) {
+    while (b >= t.first[k + 1]) k++;
+    const AdamRow& row = t.row[k];
+    const unsigned block = b - t.first[k];
+    if ((row.flags & 1) && (unsigned long long)(block + 1) * kBlock <= row.n) tensor_block<GT, W, STATE, true>(row, s, r, block, lane);
+    else tensor_block<GT, W, STATE, false>(row, s, r, block, lane);
+  }
+}
+
+template <int GT, int W, int STATE, bool VEC>
+__device__ __forceinline__ void sharded_block(const ShardedArgs& a, const AdamScalars& s, const Rates& r, int c, unsigned block, unsigned long long lo,
+                                              unsigned long long n, int lane) {
+  const unsigned long long at = (unsigned long long)block * kBlock;
+  const unsigned left = (unsigned)min(n - at, (unsigned long long)kBlock);
+  Held<W, STATE, VEC> h;
+  h.load(a.param[c], a.master[c], a.m[c], a.v[c], a.m_scale[c], a.v_scale[c], lo + at, at, left, lane);
+  // the ring's order: c + 1, c + 2, ..., c; four ranks' gradients in flight at a time
+  float g[8];
+  for (int j0 = 0; j0 < a.R; j0 += 4) {
+    float x[4][8];
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+      if (j0 + j < a.R) {
+        int from = c + 1 + j0 + j;
+        from -= from >= a.R ? a.R : 0;
+        load_floats<GT, VEC>(a.grad[from], lo + at, left, lane, x[j]);
+      }
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+      if (j0 + j < a.R) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) g[i] = j0 + j ? __fadd_rn(g[i], x[j][i]) : x[j][i];
+      }
+  }
+  h.step(g, s, r, fmaf(-r.lr, a.decay, 1.0f), STATE == HOCCL_STATE_8BIT ? tensor_key(r.seed, (unsigned)c) : 0, a.master[c], a.m[c], a.v[c], a.m_scale[c],
+         a.v_scale[c], at, left, lane);
+  for (int to = 0; to < a.R; to++) store_floats<W == W_FP32 ? 0 : 1, VEC>(a.param[to], lo + at, left, lane, h.p);
+}
+
+template <int GT, int W, int STATE>
+__global__ void __launch_bounds__(kOptThreads) sharded_adamw_kernel(const __grid_constant__ ShardedArgs a, const __grid_constant__ AdamScalars s) {
+  wait_for_stream();
+  const Rates r = read_rates(s);
+  if (r.skip) return;
+  const int lane = threadIdx.x & 31;
+  const unsigned long long total = (unsigned long long)a.per_rank * a.R;
+  const unsigned long long b0 = ((unsigned long long)blockIdx.x * kWarps + threadIdx.x / 32) * a.per_warp;
+  for (unsigned long long b = b0; b < min(b0 + a.per_warp, total); b++) {
+    const int c = (int)(b / a.per_rank);
+    const unsigned block = (unsigned)(b - (unsigned long long)c * a.per_rank);
+    const unsigned long long lo = min(c * a.q, a.count), n = min(a.q, a.count - lo);
+    if ((unsigned long long)block * kBlock >= n) continue;   // the short chunks at the end have fewer blocks
+    if ((a.aligned >> c & 1) && (unsigned long long)(block + 1) * kBlock <= n) sharded_block<GT, W, STATE, true>(a, s, r, c, block, lo, n, lane);
+    else sharded_block<GT, W, STATE, false>(a, s, r, c, block, lo, n, lane);
+  }
+}
+
+// ---------------------------------------------------------------- device: the norm
+
+constexpr int kNormThreads = 256, kNormCtas = 8 * kAllSms, kNormTile = 4 * kNormThreads;   // vectors of 16 bytes in a tile
+struct NormRow {
+  const void* p;
+  unsigned long long n;
+};
+template <int N>
+struct NormTableT {
+  int n, first_launch;
+  double* partial;               // one for each CTA: launches of one call add to it one after the other
+  NormRow row[N];
+  unsigned first[N + 1];         // prefix sums of tiles
+};
+constexpr int kNormRows = 1024;
+using NormTableSmall = NormTableT<64>;
+using NormTable = NormTableT<kNormRows>;
+static_assert(sizeof(NormTable) <= 32764, "kernel parameters");
+
+// Squares in binary64: the square of any binary32 number is there, and a long sum keeps its bits.
+template <int DT>
+__device__ __forceinline__ double squares(uint4 r) {
+  float x[8];
+  if (DT == 1) {
+    widen8(r, x);
+  } else {
+    x[0] = __uint_as_float(r.x);
+    x[1] = __uint_as_float(r.y);
+    x[2] = __uint_as_float(r.z);
+    x[3] = __uint_as_float(r.w);
+  }
+  double s = 0;
+#pragma unroll
+  for (int i = 0; i < (DT == 1 ? 8 : 4); i++) s = fma((double)x[i], (double)x[i], s);
+  return s;
+}
+template <int DT>
+__device__ __forceinline__ double square_of(const void* p, unsigned long long i) {
+  const float x = DT == 1 ? __uint_as_float((unsigned)static_cast<const unsigned short*>(p)[i] << 16) : static_cast<const float*>(p)[i];
+  return (double)x * (double)x;
+}
+
+__device__ __forceinline__ double cta_sum(double s, double* shared) {   // in a fixed order; valid in thread 0
+#pragma unroll
+  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  if ((threadIdx.x & 31) == 0) shared[threadIdx.x / 32] = s;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    for (unsigned w = 1; w < blockDim.x / 32; w++) s += shared[w];
+  return s;
+}
+
+template <int DT, class Table>
+__global__ void __launch_bounds__(kNormThreads) norm_kernel(const __grid_constant__ Table t) {
+  using T = Traits<DT>;
+  __shared__ double shared[kNormThreads / 32];
+  wait_for_stream();
+  double sum = 0;
+  const unsigned tiles = t.first[t.n];
+  int k = 0;
+  for (unsigned tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    if (tile >= t.first[k + 1])
+      for (int step = t.n <= 64 ? 32 : 512; step; step >>= 1)
+        if (k + step < t.n && t.first[k + step] <= tile) k += step;
+    const NormRow row = t.row[k];
+    const unsigned head = min((unsigned long long)((16u - ((unsigned)(uintptr_t)row.p & 15u)) & 15u) / T::E, row.n);
+    const unsigned long long nvec = (row.n - head) / T::VE, at = (unsigned long long)(tile - t.first[k]) * kNormTile;
+    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(row.p) + (size_t)head * T::E) + at;
+    const unsigned here = at < nvec ? (unsigned)min(nvec - at, (unsigned long long)kNormTile) : 0;
+    uint4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; u++) v[u] = threadIdx.x + u * kNormThreads < here ? __ldcs(p + threadIdx.x + u * kNormThreads) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int u = 0; u < 4; u++) sum += squares<DT>(v[u]);
+    const unsigned ends = (unsigned)(row.n - nvec * T::VE);   // elements before and behind the vectors
+    if (at == 0 && threadIdx.x < ends) sum += square_of<DT>(row.p, threadIdx.x < head ? threadIdx.x : nvec * T::VE + threadIdx.x);
+  }
+  sum = cta_sum(sum, shared);
+  if (threadIdx.x == 0) t.partial[blockIdx.x] = t.first_launch ? sum : t.partial[blockIdx.x] + sum;
+}
+
+struct NormEndArgs {
+  const double* partial;
+  int n;
+  double max_norm;
+  float* out;
+};
+__global__ void __launch_bounds__(kNormThreads) norm_end_kernel(const __grid_constant__ NormEndArgs a) {
+  __shared__ double shared[kNormThreads / 32];
+  wait_for_stream();
+  double s = 0;
+  for (int i = threadIdx.x; i < a.n; i += kNormThreads) s += a.partial[i];
+  s = cta_sum(s, shared);
+  if (threadIdx.x == 0) {
+    const double norm = sqrt(s);
+    a.out[0] = (float)norm;
+    a.out[1] = isfinite(norm) ? (float)fmin(1.0, a.max_norm / (norm + 1e-6)) : __uint_as_float(0x7fc00000u);
+  }
+}
+
+// ---------------------------------------------------------------- host: dispatch
+
+template <class Table>
+const void* adamw_entry(int gt, int w, int state) {
+#define ROW(G, W) {reinterpret_cast<const void*>(&adamw_kernel<G, W, 0, Table>), reinterpret_cast<const void*>(&adamw_kernel<G, W, 1, Table>)}
+  static const void* const fns[2][3][2] = {{ROW(0, 0), ROW(0, 1), ROW(0, 2)}, {ROW(1, 0), ROW(1, 1), ROW(1, 2)}};
+#undef ROW
+  return fns[gt][w][state];
+}
+const void* sharded_entry(int gt, int w, int state) {
+#define ROW(G, W) {reinterpret_cast<const void*>(&sharded_adamw_kernel<G, W, 0>), reinterpret_cast<const void*>(&sharded_adamw_kernel<G, W, 1>)}
+  static const void* const fns[2][3][2] = {{ROW(0, 0), ROW(0, 1), ROW(0, 2)}, {ROW(1, 0), ROW(1, 1), ROW(1, 2)}};
+#undef ROW
+  return fns[gt][w][state];
+}
+const void* norm_entry(int dtype, bool small) {
+  if (small) return dtype ? reinterpret_cast<const void*>(&norm_kernel<1, NormTableSmall>) : reinterpret_cast<const void*>(&norm_kernel<0, NormTableSmall>);
+  return dtype ? reinterpret_cast<const void*>(&norm_kernel<1, NormTable>) : reinterpret_cast<const void*>(&norm_kernel<0, NormTable>);
+}
+
+// Blocks of one warp: one while the whole GPU has warps to spare for that, then as many as keep the launch at 16 waves.
+unsigned blocks_per_warp(unsigned long long blocks) {
+  const unsigned long long wave = (unsigned long long)kAllSms * 32;
+  return (unsigned)std::min<unsigned long long>(std::max<unsigned long long>(blocks / (16 * wave), 1), 1u << 20);
+}
+bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+bool fill_scalars(const hoccl_adamw_config_t& c, AdamScalars* s) {
+  for (double x : {c.lr, c.beta1, c.beta2, c.eps, c.grad_scale})
+    if (!std::isfinite(x)) return false;
+  if (c.beta1 < 0 || c.beta1 >= 1 || c.beta2 < 0 || c.beta2 >= 1 || !(c.eps > 0) || c.step < 1) return false;
+  if (!aligned_to(c.factor, 4) || !aligned_to(c.rates, 16)) return false;
+  // 1 - beta^t by way of the logarithm: no cancellation for beta near 1; beta = 0 gives 1
+  const double bias1 = -std::expm1((double)c.step * std::log(c.beta1)), bias2 = -std::expm1((double)c.step * std::log(c.beta2));
+  s->lr = (float)c.lr;
+  s->step_size = (float)(c.lr / bias1);
+  s->root_scale = (float)(1.0 / std::sqrt(bias2));
+  s->beta1 = (float)c.beta1;
+  s->grad1 = (float)(1.0 - c.beta1);
+  s->beta2 = (float)c.beta2;
+  s->grad2 = (float)(1.0 - c.beta2);
+  s->eps = (float)c.eps;
+  s->grad_scale = (float)c.grad_scale;
+  s->seed = c.seed;
+  s->factor = c.factor;
+  s->rates = c.rates;
+  return s->eps > 0;
+}
+
+struct Region {
+  const char* at;
+  size_t bytes;
+  bool written;
+};
+// Whether a region that is written overlaps any other one.
+bool regions_clash(std::vector<Region>* regions) {
+  std::sort(regions->begin(), regions->end(), [](const Region& a, const Region& b) { return a.at < b.at; });
+  const char *end = nullptr, *written_end = nullptr;   // of what came before
+  for (const Region& r : *regions) {
+    if (!r.bytes) continue;
+    if (r.at < written_end || (r.written && r.at < end)) return true;
+    end = std::max(end, r.at + r.bytes);
+    if (r.written) written_end = std::max(written_end, r.at + r.bytes);
+  }
+  return false;
+}
+
+// Checks one tensor's (shard's) state and adds its regions; *aligned is cleared if an array does not start on an access of eight elements.
+bool state_fits(const void* m, const void* v, const float* master, const float* ms, const float* vs, size_t n, int state, std::vector<Region>* regions, bool* aligned) {
+  const size_t e = state == HOCCL_STATE_FLOAT32 ? 4 : 1;
+  if (!m || !v || !aligned_to(m, e) || !aligned_to(v, e) || !aligned_to(master, 4)) return false;
+  *aligned = *aligned && aligned_to(m, 8 * e) && aligned_to(v, 8 * e) && aligned_to(master, 32);
+  regions->push_back({(const char*)m, n * e, true});
+  regions->push_back({(const char*)v, n * e, true});
+  if (master) regions->push_back({(const char*)master, n * 4, true});
+  if (state == HOCCL_STATE_8BIT) {
+    if (!ms || !vs || !aligned_to(ms, 4) || !aligned_to(vs, 4)) return false;
+    const size_t bytes = (n + kBlock - 1) / kBlock * 4;
+    regions->push_back({(const char*)ms, bytes, true});
+    regions->push_back({(const char*)vs, bytes, true});
+  }
+  return true;
+}
+
+}  // namespace
+
+void add_optim_kernels(std::vector<const void*>* fns) {
+  for (int gt = 0; gt < 2; gt++) {
+    for (int w = 0; w < 3; w++)
+      for (int state = 0; state < 2; state++)
+        for (const void* f : {adamw_entry<AdamTableSmall>(gt, w, state), adamw_entry<AdamTable>(gt, w, state), sharded_entry(gt, w, state)}) fns->push_back(f);
+    for (bool small : {false, true}) fns->push_back(norm_entry(gt, small));
+  }
+  fns->push_back(reinterpret_cast<const void*>(&norm_end_kernel));
+}
+
+}  // namespace hoccl
+
+// Tables ready to launch.
+struct hoccl_adamw_plan {
+  int grad_dtype, weights, state;
+  std::vector<AdamTableSmall> small;
+  std::vector<AdamTable> large;
+};
+
+namespace {
+
+constexpr size_t kMaxTensorElements = 1ull << 39;   // blocks are counted in 32 bits
+
+template <class Table>
+void append_table(const std::vector<AdamRow>& rows, size_t from, size_t n, std::vector<Table>* out) {
+  out->emplace_back();
+  Table& t = out->back();
+  t.n = (int)n;
+  t.pad = 0;
+  t.blocks = 0;
+  for (size_t k = 0; k < n; k++) {
+    t.row[k] = rows[from + k];
+    t.first[k] = t.blocks;
+    t.blocks += (unsigned)((t.row[k].n + kBlock - 1) / kBlock);
+  }
+  t.first[n] = t.blocks;
+  t.per_warp = blocks_per_warp(t.blocks);
+}
+
+hoccl_result_t make_plan(hoccl_adamw_plan_t* out, const hoccl_adamw_tensor_t* tensors, int n, int param_dtype, int grad_dtype, int state) {
+  const size_t pe = dtype_size(param_dtype), ge = dtype_size(grad_dtype);
+  std::vector<AdamRow> rows;
+  std::vector<Region> regions;
+  bool with = false, without = false;
+  for (int k = 0; k < n; k++) {
+    const hoccl_adamw_tensor_t& t = tensors[k];
+    if (t.count == 0) continue;
+    if (t.count > kMaxTensorElements || !t.param || !t.grad || !aligned_to(t.param, pe) || !aligned_to(t.grad, ge) || !std::isfinite(t.weight_decay)) return HOCCL_ERR_INVALID_ARG;
+    (t.master ? with : without) = true;
+    bool aligned = aligned_to(t.param, 8 * pe) && aligned_to(t.grad, 8 * ge);
+    if (!state_fits(t.exp_avg, t.exp_avg_sq, t.master, t.exp_avg_scale, t.exp_avg_sq_scale, t.count, state, &regions, &aligned)) return HOCCL_ERR_INVALID_ARG;
+    regions.push_back({(const char*)t.param, t.count * pe, true});
+    regions.push_back({(const char*)t.grad, t.count * ge, false});
+    rows.push_back(AdamRow{t.param, t.exp_avg, t.exp_avg_sq, t.grad, t.master, t.exp_avg_scale, t.exp_avg_sq_scale, (unsigned long long)t.count, t.weight_decay,
+                           (unsigned)k << 1 | (aligned ? 1u : 0u)});
+  }
+  if (with && without) return HOCCL_ERR_INVALID_ARG;
+  if (with && param_dtype != HOCCL_BFLOAT16) return HOCCL_ERR_UNSUPPORTED;
+  if (regions_clash(&regions)) return HOCCL_ERR_INVALID_ARG;
+  hoccl_adamw_plan* p = new hoccl_adamw_plan();
+  *out = p;   // the caller frees it if filling it runs out of memory
+  p->grad_dtype = grad_dtype;
+  p->state = state;
+  p->weights = param_dtype == HOCCL_FLOAT32 ? W_FP32 : with ? W_MASTER : W_BF16;
+  constexpr size_t kLarge = sizeof(AdamTable::row) / sizeof(AdamRow), kSmall = sizeof(AdamTableSmall::row) / sizeof(AdamRow);
+  for (size_t from = 0; from < rows.size();) {
+    unsigned long long blocks = 0;
+    size_t here = 0;   // as many as a table and 32 bits of blocks hold
+    while (here < kLarge && from + here < rows.size()) {
+      const unsigned long long more = (rows[from + here].n + kBlock - 1) / kBlock;
+      if (here && blocks + more > 1ull << 31) break;
+      blocks += more;
+      here++;
+    }
+    if (here <= kSmall) append_table(rows, from, here, &p->small);
+    else append_table(rows, from, here, &p->large);
+    from += here;
+  }
+  return HOCCL_OK;
+}
+
+template <class Table>
+cudaError_t launch_tables(const std::vector<Table>& tables, const hoccl_adamw_plan& p, AdamScalars* s, cudaStream_t stream) {
+  for (const Table& t : tables) {
+    void* params[2] = {const_cast<Table*>(&t), s};
+    const unsigned long long warps = (t.blocks + t.per_warp - 1) / t.per_warp;
+    const cudaError_t e = launch_in_order_params(adamw_entry<Table>(p.grad_dtype, p.weights, p.state), (int)((warps + kWarps - 1) / kWarps), kOptThreads, params, stream);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+bool known_state(int state) { return state == HOCCL_STATE_FLOAT32 || state == HOCCL_STATE_8BIT; }
+
+}  // namespace
+
+extern "C" {
+
+hoccl_result_t hoccl_adamw_create(hoccl_adamw_plan_t* plan, const hoccl_adamw_tensor_t* tensors, int n, hoccl_dtype_t param_dtype, hoccl_dtype_t grad_dtype,
+                                  hoccl_state_t state) {
+  if (!plan) return HOCCL_ERR_INVALID_ARG;
+  *plan = nullptr;
+  if (n < 0 || (n && !tensors)) return HOCCL_ERR_INVALID_ARG;
+  if (!dtype_size((int)param_dtype) || !dtype_size((int)grad_dtype) || !known_state((int)state)) return HOCCL_ERR_UNSUPPORTED;
+  hoccl_result_t rc;
+  try {
+    rc = make_plan(plan, tensors, n, (int)param_dtype, (int)grad_dtype, (int)state);
+  } catch (const std::bad_alloc&) {
+    rc = HOCCL_ERR_INTERNAL;
+  }
+  if (rc != HOCCL_OK) {
+    delete *plan;
+    *plan = nullptr;
+  }
+  return rc;
+}
+
+void hoccl_adamw_destroy(hoccl_adamw_plan_t plan) { delete plan; }
+
+hoccl_result_t hoccl_adamw_step(hoccl_adamw_plan_t plan, const hoccl_adamw_config_t* config, hoccl_comm_t c, hoccl_stream_t stream) {
+  const double t0 = now_us();
+  AdamScalars s;
+  if (!plan || !config || !c || !fill_scalars(*config, &s)) return HOCCL_ERR_INVALID_ARG;
+  c->stats = hoccl_stats_t{};
+  DeviceScope scope(c->device);
+  CU_TRY(c, scope.err);
+  CU_TRY(c, launch_tables(plan->small, *plan, &s, (cudaStream_t)stream));
+  CU_TRY(c, launch_tables(plan->large, *plan, &s, (cudaStream_t)stream));
+  c->stats.host_launch_us = now_us() - t0;
+  return HOCCL_OK;
+}
+
+hoccl_result_t hoccl_sharded_adamw(const void* const* grads, void* const* params, void* const* exp_avg, void* const* exp_avg_sq, float* const* master,
+                                   float* const* exp_avg_scale, float* const* exp_avg_sq_scale, size_t count, hoccl_dtype_t param_dtype,
+                                   hoccl_dtype_t grad_dtype, hoccl_state_t state, float weight_decay, const hoccl_adamw_config_t* config, hoccl_comm_t c,
+                                   hoccl_stream_t stream) {
+  const double t0 = now_us();
+  AdamScalars s;
+  const size_t pe = dtype_size((int)param_dtype), ge = dtype_size((int)grad_dtype);
+  const bool eight = state == HOCCL_STATE_8BIT;
+  if (!c || !config || !grads || !params || !exp_avg || !exp_avg_sq || (eight && (!exp_avg_scale || !exp_avg_sq_scale))) return HOCCL_ERR_INVALID_ARG;
+  if (!pe || !ge || !known_state((int)state) || (master && param_dtype != HOCCL_BFLOAT16)) return HOCCL_ERR_UNSUPPORTED;
+  if (!fill_scalars(*config, &s) || !std::isfinite(weight_decay) || count > kMaxTensorElements) return HOCCL_ERR_INVALID_ARG;
+  c->stats = hoccl_stats_t{};
+  if (count == 0) return HOCCL_OK;
+  ShardedArgs a = {};
+  a.R = c->R;
+  a.decay = weight_decay;
+  a.count = count;
+  a.q = (count + (size_t)c->R - 1) / (size_t)c->R;
+  a.per_rank = (unsigned)((a.q + kBlock - 1) / kBlock);
+  a.per_warp = blocks_per_warp((unsigned long long)a.per_rank * a.R);
+  try {
+    std::vector<Region> regions;
+    for (int r = 0; r < c->R; r++) {
+      if (!grads[r] || !params[r] || !aligned_to(grads[r], ge) || !aligned_to(params[r], pe)) return HOCCL_ERR_INVALID_ARG;
+      a.grad[r] = grads[r];
+      a.param[r] = params[r];
+      regions.push_back({(const char*)grads[r], count * ge, false});
+      regions.push_back({(const char*)params[r], count * pe, true});
+      const size_t lo = std::min((size_t)(r * a.q), count), n = std::min((size_t)a.q, count - lo);
+      if (!n) continue;
+      a.m[r] = exp_avg[r];
+      a.v[r] = exp_avg_sq[r];
+      a.master[r] = master ? master[r] : nullptr;
+      a.m_scale[r] = eight ? exp_avg_scale[r] : nullptr;
+      a.v_scale[r] = eight ? exp_avg_sq_scale[r] : nullptr;
+      bool aligned = true;
+      if ((master && !master[r]) || !state_fits(a.m[r], a.v[r], a.master[r], a.m_scale[r], a.v_scale[r], n, (int)state, &regions, &aligned)) return HOCCL_ERR_INVALID_ARG;
+      for (int k = 0; k < c->R; k++) aligned = aligned && aligned_to((const char*)grads[k] + lo * ge, 8 * ge) && aligned_to((const char*)params[k] + lo * pe, 8 * pe);
+      if (aligned) a.aligned |= 1ull << r;
+    }
+    if (regions_clash(&regions)) return HOCCL_ERR_INVALID_ARG;
+  } catch (const std::bad_alloc&) {
+    return HOCCL_ERR_INTERNAL;
+  }
+  DeviceScope scope(c->device);
+  CU_TRY(c, scope.err);
+  const unsigned long long warps = ((unsigned long long)a.per_rank * a.R + a.per_warp - 1) / a.per_warp;
+  void* launch[2] = {&a, &s};
+  const int weights = param_dtype == HOCCL_FLOAT32 ? W_FP32 : master ? W_MASTER : W_BF16;
+  CU_TRY(c, launch_in_order_params(sharded_entry((int)grad_dtype, weights, (int)state), (int)((warps + kWarps - 1) / kWarps), kOptThreads, launch, (cudaStream_t)stream));
+  c->stats.host_launch_us = now_us() - t0;
+  return HOCCL_OK;
+}
+
+size_t hoccl_grad_norm_scratch_bytes(void) { return kNormCtas * sizeof(double); }
+
+}  // extern "C"
+
+namespace {
+
+// Launches one table of vectors after the other; all launches of a call have the same grid, so that CTA b adds to partial b in order.
+template <class Table>
+cudaError_t norm_launches(const std::vector<NormRow>& rows, size_t cap, int dtype, int grid, double* partial, cudaStream_t stream) {
+  Table t;
+  for (size_t from = 0; from < rows.size() || from == 0; from += cap) {
+    t.n = (int)std::min(cap, rows.size() - from);
+    t.first_launch = from == 0;
+    t.partial = partial;
+    t.first[0] = 0;
+    const size_t e = dtype_size(dtype);
+    for (int k = 0; k < t.n; k++) {
+      t.row[k] = rows[from + k];
+      t.first[k + 1] = t.first[k] + (unsigned)std::max<unsigned long long>((t.row[k].n * e / 16 + kNormTile - 1) / kNormTile, 1);
+    }
+    const cudaError_t err = launch_in_order(norm_entry(dtype, sizeof(Table) == sizeof(NormTableSmall)), grid, kNormThreads, &t, stream);
+    if (err != cudaSuccess) return err;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace
+
+extern "C" hoccl_result_t hoccl_grad_norm(const void* const* grads, const size_t* counts, int n, hoccl_dtype_t dtype, double max_norm, float* out, hoccl_comm_t c,
+                                          hoccl_stream_t stream) {
+  const double t0 = now_us();
+  const size_t e = dtype_size((int)dtype);
+  if (!c || !out || n < 0 || (n && (!grads || !counts)) || !aligned_to(out, 4) || !(max_norm > 0)) return HOCCL_ERR_INVALID_ARG;
+  if (!e) return HOCCL_ERR_UNSUPPORTED;
+  try {
+    std::vector<NormRow> rows;
+    unsigned long long tiles = 0;
+    for (int k = 0; k < n; k++) {
+      if (!counts[k]) continue;
+      if (!grads[k] || !aligned_to(grads[k], e) || counts[k] > kMaxTensorElements) return HOCCL_ERR_INVALID_ARG;
+      rows.push_back(NormRow{grads[k], (unsigned long long)counts[k]});
+      tiles += (counts[k] * e / 16 + kNormTile - 1) / kNormTile + 1;
+    }
+    if (tiles >= 1ull << 32) return HOCCL_ERR_INVALID_ARG;
+    if (!c->scratch || c->scratch_bytes < hoccl_grad_norm_scratch_bytes()) return HOCCL_ERR_SCRATCH;
+    c->stats = hoccl_stats_t{};
+    DeviceScope scope(c->device);
+    CU_TRY(c, scope.err);
+    const int grid = (int)std::min<unsigned long long>(std::max<unsigned long long>(tiles, 1), kNormCtas);
+    double* partial = static_cast<double*>(c->scratch);
+    if (rows.size() <= 64) CU_TRY(c, norm_launches<NormTableSmall>(rows, 64, (int)dtype, grid, partial, (cudaStream_t)stream));
+    else CU_TRY(c, norm_launches<NormTable>(rows, kNormRows, (int)dtype, grid, partial, (cudaStream_t)stream));
+    NormEndArgs end{partial, grid, max_norm, out};
+    CU_TRY(c, launch_in_order(reinterpret_cast<const void*>(&norm_end_kernel), 1, kNormThreads, &end, (cudaStream_t)stream));
+  } catch (const std::bad_alloc&) {
+    return HOCCL_ERR_INTERNAL;
+  }
+  c->stats.host_launch_us = now_us() - t0;
+  return HOCCL_OK;
+}

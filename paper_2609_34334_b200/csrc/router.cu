@@ -1,0 +1,647 @@
+// The router of an expert-parallel layer: softmax, the topk experts of each token, their counts (which an all-to-allv is made of) and the
+// balance loss, forward and backward.  (The paper has no counterpart.)
+//
+// A row of logits is held by L lanes with V logits each, in registers, for all that is done with it: one read of the logits, no second pass.  Sums over
+// the tokens (the probability of each expert, how often it was chosen) stay in a lane's registers and the CTA's shared memory until the CTA has done its rows;
+// its sums then go to scratch and one cluster of CTAs adds them in a fixed order, so that the same call gives the same bits.
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "comm.h"
+#include "device_common.cuh"
+
+using namespace hoccl;
+
+namespace hoccl {
+namespace {
+
+constexpr int kMaxExperts = 1024, kMaxTopk = 32;
+constexpr int kRouteThreads = 256, kRouteWarps = kRouteThreads / 32;
+constexpr int kRouteCtas = 4 * kAllSms;          // CTAs of a forward launch besides one for each rank: bounds the scratch
+constexpr int kEndCtas = 8;                      // one cluster
+
+struct RouteArgs {
+  int R, experts, topk, groups;
+  unsigned long long ld, dld;
+  unsigned rows_per_cta;
+  int normalize;
+  float* partial;                // forward: 2 * experts + 2 words for each CTA: sums of p, counts, rows, sum of squared logarithms
+  const float* saved;            // backward
+  const float* dloss;
+  unsigned first[kMaxRanks + 1]; // prefix sums of CTAs
+  unsigned tokens[kMaxRanks];
+  const void* logits[kMaxRanks];
+  int* indices[kMaxRanks];
+  float* weights[kMaxRanks];     // backward: their gradients
+  void* dlogits[kMaxRanks];
+};
+struct RouteEndArgs {
+  int R, experts, topk, groups;
+  double balance, z;             // balance_coef * experts, z_coef
+  const float* partial;
+  float *loss, *saved;
+  unsigned first[kMaxRanks + 1];
+  int* counts[kMaxRanks];
+};
+
+// A number as an unsigned word of the same order; +0 and -0 alike; NaN below everything.
+__device__ __forceinline__ unsigned order_key(float x) {
+  const unsigned b = __float_as_uint(x + 0.0f);
+  return x != x ? 0u : b ^ ((int)b < 0 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float from_order_key(unsigned k) { return __uint_as_float(k ^ ((int)k < 0 ? 0x80000000u : 0xffffffffu)); }
+constexpr unsigned kClosedKey = 0x007fffffu;   // of -infinity: such an expert is not chosen
+
+template <int L>
+__device__ __forceinline__ float lanes_max(float x) {
+#pragma unroll
+  for (int d = L / 2; d; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+  return x;
+}
+template <int L>
+__device__ __forceinline__ float lanes_sum(float x) {
+#pragma unroll
+  for (int d = L / 2; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+  return x;
+}
+template <int L>
+__device__ __forceinline__ unsigned lanes_max(unsigned x) {
+  if constexpr (L == 32) {
+    return __reduce_max_sync(0xffffffffu, x);
+  } else {
+#pragma unroll
+    for (int d = L / 2; d; d >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, d));
+    return x;
+  }
+}
+template <int L>
+__device__ __forceinline__ unsigned lanes_min(unsigned x) {
+  if constexpr (L == 32) {
+    return __reduce_min_sync(0xffffffffu, x);
+  } else {
+#pragma unroll
+    for (int d = L / 2; d; d >>= 1) x = min(x, __shfl_xor_sync(0xffffffffu, x, d));
+    return x;
+  }
+}
+
+// Which expert lane `lane`'s i-th logit belongs to.  VEC (rows that are whole, aligned vectors): V consecutive ones; else spread for coalescing.
+template <int V, int L, bool VEC>
+__device__ __forceinline__ int expert_of(int lane, int i) {
+  return VEC ? lane * V + i : i * L + lane;
+}
+
+template <int DT, int V, int L, bool VEC>
+__device__ __forceinline__ void load_row(const void* base, unsigned long long at, int experts, int lane, float* x) {
+  if (VEC) {
+    constexpr int VE = Traits<DT>::VE;
+    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(base) + at * Traits<DT>::E);
+#pragma unroll
+    for (int j = 0; j < V / VE; j++) {
+      const bool in = (lane * V + j * VE) < experts;
+      const uint4 r = in ? __ldcs(p + lane * (V / VE) + j) : make_uint4(0, 0, 0, 0);
+      const unsigned w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        if (DT == 0) {
+          x[j * VE + i] = in ? __uint_as_float(w[i]) : -INFINITY;
+        } else {
+          x[j * VE + 2 * i] = in ? __uint_as_float(w[i] << 16) : -INFINITY;
+          x[j * VE + 2 * i + 1] = in ? __uint_as_float(w[i] & 0xffff0000u) : -INFINITY;
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+      const int e = expert_of<V, L, VEC>(lane, i);
+      if (DT == 0) x[i] = e < experts ? __ldcs(static_cast<const float*>(base) + at + e) : -INFINITY;
+      else x[i] = e < experts ? __uint_as_float((unsigned)__ldcs(static_cast<const unsigned short*>(base) + at + e) << 16) : -INFINITY;
+    }
+  }
+}
+
+// x -> exp(x - top) / their sum; the logarithm of the sum of exp(x).  A row without a logit above -infinity: probabilities 0, NaN where
+// the logit is, logarithm 0.  top and inv: p of a logit y of this row is exp(y - top) * inv.
+template <int V, int L>
+__device__ __forceinline__ void softmax_row(float* x, float* log_sum, float* top_out, float* inv_out) {
+  float top = x[0];
+#pragma unroll
+  for (int i = 1; i < V; i++) top = fmaxf(top, x[i]);
+  top = lanes_max<L>(top);
+  const bool open = top > -INFINITY;
+  if (!open) top = 0.0f;
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < V; i++) sum += x[i] = __expf(x[i] - top);
+  sum = lanes_sum<L>(sum);
+  const float inv = open ? 1.0f / sum : 1.0f;
+#pragma unroll
+  for (int i = 0; i < V; i++) x[i] *= inv;
+  *log_sum = open ? top + logf(sum) : 0.0f;
+  *top_out = top;
+  *inv_out = inv;
+}
+
+template <int DT, int V, int L, bool VEC>
+__global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_constant__ RouteArgs a) {
+  constexpr int G = 32 / L, kRows = kRouteWarps * G;   // rows of a warp, of the CTA, at a time
+  constexpr int K = L * V < kMaxTopk ? L * V : kMaxTopk;
+  extern __shared__ float sums[];                      // [kRouteWarps][experts] at the end
+  __shared__ int count[L * V + 1];
+  __shared__ unsigned chosen_key[kRows][K];
+  __shared__ int chosen[kRows][K];
+  __shared__ float squares[kRouteWarps];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % L, group = threadIdx.x % 32 / L, slot = warp * G + group;
+  for (int e = threadIdx.x; e <= a.experts; e += kRouteThreads) count[e] = 0;
+  int r = 0;
+  while (blockIdx.x >= a.first[r + 1]) r++;
+  const unsigned row0 = (blockIdx.x - a.first[r]) * a.rows_per_cta, row1 = min(a.tokens[r], row0 + a.rows_per_cta);
+  wait_for_stream();
+  __syncthreads();
+  float p_sum[V] = {}, z_sum = 0.0f;
+  for (unsigned base = row0 + warp * G; base < row1; base += kRows) {
+    const unsigned row = base + group;
+    const bool real = row < row1;
+    float x[V], log_sum, top, inv;
+    if (real) {
+      load_row<DT, V, L, VEC>(a.logits[r], row * a.ld, a.experts, lane, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; i++) x[i] = -INFINITY;
+    }
+    unsigned key[V];
+#pragma unroll
+    for (int i = 0; i < V; i++) key[i] = order_key(x[i]);
+    softmax_row<V, L>(x, &log_sum, &top, &inv);
+#pragma unroll
+    for (int i = 0; i < V; i++) p_sum[i] += x[i];
+    z_sum += log_sum * log_sum;
+    float sel_sum = 0.0f;
+    for (int k = 0; k < a.topk; k++) {
+      unsigned best = key[0];
+#pragma unroll
+      for (int i = 1; i < V; i++) best = max(best, key[i]);
+      best = lanes_max<L>(best);
+      int mine = -1;
+#pragma unroll
+      for (int i = V - 1; i >= 0; i--)
+        if (key[i] == best) mine = i;                  // the lowest of this lane's
+      const unsigned e = lanes_min<L>(mine >= 0 ? (unsigned)expert_of<V, L, VEC>(lane, mine) : 0xffffffffu);
+      const bool found = best > kClosedKey;
+#pragma unroll
+      for (int i = 0; i < V; i++)
+        if (found && (unsigned)expert_of<V, L, VEC>(lane, i) == e) key[i] = 0;
+      if (lane == 0) {
+        chosen_key[slot][k] = best;
+        chosen[slot][k] = found ? (int)e : -1;
+        if (found) atomicAdd(&count[e], 1);
+      }
+      if (found) sel_sum += __expf(from_order_key(best) - top);
+    }
+    if (lane == 0 && chosen[slot][0] >= 0) atomicAdd(&count[a.experts], 1);
+    __syncwarp();
+    if (real) {
+      const float scale = a.normalize ? 1.0f / sel_sum + 0.0f * inv : inv;   // a NaN in the row reaches its weights either way
+      for (int k = lane; k < a.topk; k += L) {
+        const int e = chosen[slot][k];
+        const unsigned long long at = (unsigned long long)row * a.topk + k;
+        a.indices[r][at] = e;
+        a.weights[r][at] = e < 0 ? 0.0f : __expf(from_order_key(chosen_key[slot][k]) - top) * scale;
+      }
+    }
+    __syncwarp();
+  }
+  // the CTA's sums: lanes of one expert, then warps, in order
+#pragma unroll
+  for (int i = 0; i < V; i++) {
+#pragma unroll
+    for (int d = L; d < 32; d <<= 1) p_sum[i] += __shfl_xor_sync(0xffffffffu, p_sum[i], d);
+    const int e = expert_of<V, L, VEC>(lane, i);
+    if (group == 0 && e < a.experts) sums[warp * a.experts + e] = p_sum[i];
+  }
+#pragma unroll
+  for (int d = L; d < 32; d <<= 1) z_sum += __shfl_xor_sync(0xffffffffu, z_sum, d);
+  if (threadIdx.x % 32 == 0) squares[warp] = z_sum;
+  __syncthreads();
+  float* out = a.partial + (size_t)blockIdx.x * (2 * a.experts + 2);
+  for (int e = threadIdx.x; e < a.experts; e += kRouteThreads) {
+    float s = 0.0f;
+    for (int w = 0; w < kRouteWarps; w++) s += sums[w * a.experts + e];
+    out[e] = s;
+    out[a.experts + e] = __int_as_float(count[e]);
+  }
+  if (threadIdx.x == 0) {
+    float z = 0.0f;
+    for (int w = 0; w < kRouteWarps; w++) z += squares[w];
+    out[2 * a.experts] = __int_as_float(count[a.experts]);
+    out[2 * a.experts + 1] = z;
+  }
+}
+
+// Adds the CTAs' sums.  One cluster; each CTA takes 32 experts at a time (a lane each, the warps share the forward CTAs), the first CTA
+// adds the parts of the loss.
+__global__ void __cluster_dims__(kEndCtas, 1, 1) __launch_bounds__(1024) route_end_kernel(const __grid_constant__ RouteEndArgs a) {
+  namespace cg = cooperative_groups;
+  __shared__ double p_part[32][33];
+  __shared__ int c_part[32][33];
+  __shared__ int rows[kMaxRanks];
+  __shared__ double logs[kMaxRanks], loss[kMaxRanks];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  cg::cluster_group cluster = cg::this_cluster();
+  wait_for_stream();
+  const size_t words = 2 * (size_t)a.experts + 2;
+  for (int r = warp; r < a.R; r += 32) {   // every CTA needs the ranks' rows
+    int n = 0;
+    double z = 0;
+    for (unsigned b = a.first[r] + lane; b < a.first[r + 1]; b += 32) {
+      n += __float_as_int(__ldcg(a.partial + b * words + 2 * a.experts));
+      z += __ldcg(a.partial + b * words + 2 * a.experts + 1);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+      n += __shfl_xor_sync(0xffffffffu, n, d);
+      z += __shfl_xor_sync(0xffffffffu, z, d);
+    }
+    if (lane == 0) {
+      rows[r] = n;
+      logs[r] = z;
+    }
+  }
+  if (threadIdx.x < kMaxRanks) loss[threadIdx.x] = 0;
+  __syncthreads();
+  long long all = 0;
+  for (int r = 0; r < a.R; r++) all += rows[r];
+  for (int e0 = 32 * blockIdx.x; e0 < a.experts; e0 += 32 * kEndCtas) {
+    const int e = e0 + lane;
+    double p_all = 0;
+    long long c_all = 0;
+    for (int r = 0; r < a.R; r++) {
+      double p = 0;
+      int n = 0;
+      if (e < a.experts)
+        for (unsigned b = a.first[r] + warp; b < a.first[r + 1]; b += 32) {
+          p += __ldcg(a.partial + b * words + e);
+          n += __float_as_int(__ldcg(a.partial + b * words + a.experts + e));
+        }
+      __syncthreads();
+      p_part[warp][lane] = p;
+      c_part[warp][lane] = n;
+      __syncthreads();
+      if (warp == 0) {
+        p = 0;
+        n = 0;
+        for (int w = 0; w < 32; w++) {
+          p += p_part[w][lane];
+          n += c_part[w][lane];
+        }
+        if (e < a.experts) a.counts[r][e] = n;
+        p_all += p;
+        c_all += n;
+        if (a.groups > 1 || r == a.R - 1) {   // a group ends here
+          const int g = a.groups > 1 ? r : 0;
+          const double rows_here = a.groups > 1 ? rows[r] : (double)all, f = rows_here > 0 ? c_all / (a.topk * rows_here) : 0;
+          if (e < a.experts) a.saved[(size_t)g * (a.experts + 1) + e] = (float)(rows_here > 0 ? a.balance * f / rows_here : 0);
+          double part = rows_here > 0 ? f * p_all / rows_here : p_all;   // no rows: 0, or NaN
+#pragma unroll
+          for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
+          if (lane == 0) loss[g] += part;
+          p_all = 0;
+          c_all = 0;
+        }
+      }
+    }
+  }
+  cluster.sync();
+  if (blockIdx.x == 0) {
+    for (int r = threadIdx.x; r < a.R; r += 1024) a.counts[r][a.experts] = rows[r];
+    for (int g = threadIdx.x; g < a.groups; g += 1024) {
+      double n = a.groups > 1 ? rows[g] : (double)all, z = logs[g], l = 0;
+      if (a.groups == 1)
+        for (int r = 1; r < a.R; r++) z += logs[r];
+      for (int c = 0; c < kEndCtas; c++) l += *cluster.map_shared_rank(&loss[g], c);
+      a.loss[2 * g] = (float)(a.balance * l);
+      a.loss[2 * g + 1] = (float)(n > 0 ? a.z * z / n : 0);
+      a.saved[(size_t)g * (a.experts + 1) + a.experts] = (float)(n > 0 ? 2 * a.z / n : 0);
+    }
+  }
+  cluster.sync();   // the others' shared memory lives until it has been read
+}
+
+template <int DT, int V, int L, bool VEC>
+__global__ void __launch_bounds__(kRouteThreads) route_backward_kernel(const __grid_constant__ RouteArgs a) {
+  constexpr int G = 32 / L, kRows = kRouteWarps * G;
+  __shared__ float extra[kRows][L * V];   // by expert: what the weights' gradient adds
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % L, group = threadIdx.x % 32 / L, slot = warp * G + group;
+  int r = 0;
+  while (blockIdx.x >= a.first[r + 1]) r++;
+  const unsigned row0 = (blockIdx.x - a.first[r]) * a.rows_per_cta, row1 = min(a.tokens[r], row0 + a.rows_per_cta);
+  wait_for_stream();
+  const int g = a.groups > 1 ? r : 0;
+  const float scale = a.dloss ? a.dloss[g] : 1.0f, z = a.saved[(size_t)g * (a.experts + 1) + a.experts] * scale;
+  float c[V];
+#pragma unroll
+  for (int i = 0; i < V; i++) {
+    const int e = expert_of<V, L, VEC>(lane, i);
+    c[i] = e < a.experts ? a.saved[(size_t)g * (a.experts + 1) + e] * scale : 0.0f;
+  }
+  for (unsigned base = row0 + warp * G; base < row1; base += kRows) {
+    const unsigned row = base + group;
+    const bool real = row < row1;
+    float x[V], log_sum, top, inv;
+    if (real) {
+      load_row<DT, V, L, VEC>(a.logits[r], row * a.ld, a.experts, lane, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; i++) x[i] = -INFINITY;
+    }
+    softmax_row<V, L>(x, &log_sum, &top, &inv);
+    float mean = 0.0f;   // of c under p
+#pragma unroll
+    for (int i = 0; i < V; i++) mean += x[i] * c[i];
+    mean = lanes_sum<L>(mean);
+    float shift = mean - z * log_sum;
+    if (a.weights[r] != nullptr) {
+#pragma unroll
+      for (int i = 0; i < V; i++) extra[slot][i * L + lane] = 0.0f;
+      __syncwarp();
+      // weights of the chosen and their gradients' mean
+      float w_sum = 0.0f, dw_sum = 0.0f;
+      for (int k = lane; k < a.topk && real; k += L) {
+        const unsigned long long at = (unsigned long long)row * a.topk + k;
+        const unsigned e = (unsigned)a.indices[r][at];
+        if (e < (unsigned)a.experts) {
+          const unsigned long long l = row * a.ld + e;
+          const float y = DT == 0 ? static_cast<const float*>(a.logits[r])[l] : __uint_as_float((unsigned)static_cast<const unsigned short*>(a.logits[r])[l] << 16);
+          const float p = __expf(y - top) * inv;
+          w_sum += p;
+          dw_sum += p * a.weights[r][at];
+        }
+      }
+      w_sum = lanes_sum<L>(w_sum);
+      dw_sum = lanes_sum<L>(dw_sum);
+      const float per = a.normalize ? (w_sum > 0.0f ? 1.0f / w_sum : w_sum) : 1.0f;
+      const float inner = dw_sum * per;
+      for (int k = 0; k < a.topk; k++) {   // one after the other: an index that comes twice adds twice
+        if (real && lane == k % L) {
+          const unsigned long long at = (unsigned long long)row * a.topk + k;
+          const unsigned e = (unsigned)a.indices[r][at];
+          if (e < (unsigned)a.experts) {
+            const unsigned long long l = row * a.ld + e;
+            const float y = DT == 0 ? static_cast<const float*>(a.logits[r])[l] : __uint_as_float((unsigned)static_cast<const unsigned short*>(a.logits[r])[l] << 16);
+            extra[slot][e] += __expf(y - top) * inv * per * (a.weights[r][at] - (a.normalize ? inner : 0.0f));
+          }
+        }
+        __syncwarp();
+      }
+      if (!a.normalize) shift += inner;
+    }
+    if (real) {
+      float d[V];
+#pragma unroll
+      for (int i = 0; i < V; i++) {
+        const int e = expert_of<V, L, VEC>(lane, i);
+        d[i] = x[i] * (c[i] - shift) + (a.weights[r] != nullptr ? extra[slot][e] : 0.0f);
+      }
+      const unsigned long long at = row * a.dld;
+      if (VEC) {
+        constexpr int VE = Traits<DT>::VE;
+        uint4* p = reinterpret_cast<uint4*>(static_cast<char*>(a.dlogits[r]) + at * Traits<DT>::E);
+#pragma unroll
+        for (int j = 0; j < V / VE; j++)
+          if (lane * V + j * VE < a.experts) {
+            uint4 o;
+            unsigned w[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+              if (DT == 0) w[i] = __float_as_uint(d[j * VE + i]);
+              else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(d[j * VE + 2 * i + 1]), "f"(d[j * VE + 2 * i]));
+            }
+            o = make_uint4(w[0], w[1], w[2], w[3]);
+            __stcs(p + lane * (V / VE) + j, o);
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+          const int e = expert_of<V, L, VEC>(lane, i);
+          if (e < a.experts) {
+            if (DT == 0) static_cast<float*>(a.dlogits[r])[at + e] = d[i];
+            else static_cast<__nv_bfloat16*>(a.dlogits[r])[at + e] = __float2bfloat16_rn(d[i]);
+          }
+        }
+      }
+    }
+    __syncwarp();
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+// Shapes: 8 logits a lane and as many lanes as the experts need, then 16 and 32 logits a lane.
+constexpr int kShapes = 8;
+int shape_of(int experts) {
+  int s = 0;
+  while ((8 << s) < experts) s++;
+  return s;
+}
+int lanes_of(int shape) { return 1 << std::min(shape, 5); }
+
+template <int DT, bool VEC>
+const void* route_entry_of(int shape, bool backward) {
+#define ROW(V, L) {reinterpret_cast<const void*>(&route_kernel<DT, V, L, VEC>), reinterpret_cast<const void*>(&route_backward_kernel<DT, V, L, VEC>)}
+  static const void* const fns[kShapes][2] = {ROW(8, 1), ROW(8, 2), ROW(8, 4), ROW(8, 8), ROW(8, 16), ROW(8, 32), ROW(16, 32), ROW(32, 32)};
+#undef ROW
+  return fns[shape][backward];
+}
+const void* route_entry(int dtype, int shape, bool vec, bool backward) {
+  if (dtype == HOCCL_FLOAT32) return vec ? route_entry_of<0, true>(shape, backward) : route_entry_of<0, false>(shape, backward);
+  return vec ? route_entry_of<1, true>(shape, backward) : route_entry_of<1, false>(shape, backward);
+}
+
+bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+struct Span {
+  const char* at;
+  size_t bytes;
+  bool written;
+};
+bool spans_clash(std::vector<Span>* v) {
+  std::sort(v->begin(), v->end(), [](const Span& a, const Span& b) { return a.at < b.at; });
+  const char *end = nullptr, *written_end = nullptr;
+  for (const Span& s : *v) {
+    if (!s.bytes) continue;
+    if (s.at < written_end || (s.written && s.at < end)) return true;
+    end = std::max(end, s.at + s.bytes);
+    if (s.written) written_end = std::max(written_end, s.at + s.bytes);
+  }
+  return false;
+}
+size_t rows_bytes(size_t rows, size_t ld, size_t width, size_t e) { return rows ? ((rows - 1) * ld + width) * e : 0; }
+
+hoccl_result_t check_config(const hoccl_comm* c, const hoccl_route_config_t* f, const void* logits, size_t ld, const size_t* tokens) {
+  if (!c || !f || !logits || !tokens) return HOCCL_ERR_INVALID_ARG;
+  if (!dtype_size((int)f->dtype)) return HOCCL_ERR_UNSUPPORTED;
+  if (f->experts < 1 || f->experts > kMaxExperts || f->topk < 1 || f->topk > kMaxTopk || f->topk > f->experts || ld < (size_t)f->experts || ld > 1ull << 31) return HOCCL_ERR_INVALID_ARG;
+  if ((f->normalize | f->per_rank) & ~1) return HOCCL_ERR_INVALID_ARG;
+  for (int r = 0; r < c->R; r++)
+    if (tokens[r] >= 1ull << 31) return HOCCL_ERR_INVALID_ARG;
+  return HOCCL_OK;
+}
+
+// Rows of one CTA and the ranks' first CTAs: as many CTAs as `most` at most, besides one for each rank, and no fewer rows in one than its warps hold.
+unsigned share_rows(const size_t* tokens, int R, int lanes, unsigned most, unsigned* rows_per_cta, unsigned* first) {
+  unsigned long long all = 0;
+  for (int r = 0; r < R; r++) all += tokens[r];
+  const unsigned long long at_once = (unsigned long long)kRouteWarps * (32 / lanes);
+  unsigned long long per = (all + most - 1) / most;
+  per = std::max((per + at_once - 1) / at_once, 1ull) * at_once;
+  *rows_per_cta = (unsigned)per;
+  first[0] = 0;
+  for (int r = 0; r < R; r++) first[r + 1] = first[r] + (unsigned)((tokens[r] + per - 1) / per);
+  return first[R];
+}
+
+}  // namespace
+
+void add_router_kernels(std::vector<const void*>* fns) {
+  for (int dtype = 0; dtype < 2; dtype++)
+    for (int shape = 0; shape < kShapes; shape++)
+      for (int form = 0; form < 4; form++) fns->push_back(route_entry(dtype, shape, form & 1, form & 2));
+  fns->push_back(reinterpret_cast<const void*>(&route_end_kernel));
+}
+
+}  // namespace hoccl
+
+extern "C" {
+
+size_t hoccl_route_scratch_bytes(int R, size_t max_tokens, int experts) {
+  if (R < 1 || R > kMaxRanks || experts < 1 || experts > kMaxExperts) return 0;
+  const size_t at_once = (size_t)kRouteWarps * (32 / lanes_of(shape_of(experts)));
+  const size_t ctas = std::min((size_t)R * ((max_tokens + at_once - 1) / at_once), (size_t)kRouteCtas + R);
+  return (ctas * (2 * (size_t)experts + 2) * sizeof(float) + 255) / 256 * 256;
+}
+
+hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* tokens, const hoccl_route_config_t* f, int32_t* const* indices,
+                           float* const* weights, int32_t* const* counts, float* loss, float* saved, hoccl_comm_t c, hoccl_stream_t stream) {
+  const double t0 = now_us();
+  hoccl_result_t rc = check_config(c, f, logits, ld, tokens);
+  if (rc != HOCCL_OK) return rc;
+  if (!indices || !weights || !counts || !loss || !saved || !aligned_to(loss, 4) || !aligned_to(saved, 4)) return HOCCL_ERR_INVALID_ARG;
+  if (!std::isfinite(f->balance_coef) || !std::isfinite(f->z_coef)) return HOCCL_ERR_INVALID_ARG;
+  const size_t e = dtype_size((int)f->dtype);
+  const int shape = shape_of(f->experts), groups = f->per_rank ? c->R : 1;
+  RouteArgs a = {};
+  RouteEndArgs end = {};
+  a.R = end.R = c->R;
+  a.experts = end.experts = f->experts;
+  a.topk = end.topk = f->topk;
+  a.groups = end.groups = groups;
+  a.ld = ld;
+  a.normalize = f->normalize;
+  bool vec = (f->experts * e) % 16 == 0 && (ld * e) % 16 == 0;
+  try {
+    std::vector<Span> spans = {{(const char*)loss, 8u * (size_t)groups, true}, {(const char*)saved, (size_t)groups * (f->experts + 1) * 4, true}};
+    for (int r = 0; r < c->R; r++) {
+      if (!counts[r] || !aligned_to(counts[r], 4)) return HOCCL_ERR_INVALID_ARG;
+      end.counts[r] = counts[r];
+      spans.push_back({(const char*)counts[r], (size_t)(f->experts + 1) * 4, true});
+      if (!tokens[r]) continue;
+      if (!logits[r] || !indices[r] || !weights[r] || !aligned_to(logits[r], e) || !aligned_to(indices[r], 4) || !aligned_to(weights[r], 4)) return HOCCL_ERR_INVALID_ARG;
+      a.tokens[r] = (unsigned)tokens[r];
+      a.logits[r] = logits[r];
+      a.indices[r] = indices[r];
+      a.weights[r] = weights[r];
+      vec = vec && aligned_to(logits[r], 16);
+      spans.push_back({(const char*)logits[r], rows_bytes(tokens[r], ld, f->experts, e), false});
+      spans.push_back({(const char*)indices[r], tokens[r] * f->topk * 4, true});
+      spans.push_back({(const char*)weights[r], tokens[r] * f->topk * 4, true});
+    }
+    if (spans_clash(&spans)) return HOCCL_ERR_INVALID_ARG;
+  } catch (const std::bad_alloc&) {
+    return HOCCL_ERR_INTERNAL;
+  }
+  const unsigned grid = share_rows(tokens, c->R, lanes_of(shape), kRouteCtas, &a.rows_per_cta, a.first);
+  const size_t need = (size_t)grid * (2 * (size_t)f->experts + 2) * sizeof(float);
+  if (need && (!c->scratch || c->scratch_bytes < need)) return HOCCL_ERR_SCRATCH;
+  std::copy(a.first, a.first + kMaxRanks + 1, end.first);
+  a.partial = static_cast<float*>(c->scratch);
+  end.partial = a.partial;
+  end.balance = f->balance_coef * f->experts;
+  end.z = f->z_coef;
+  end.loss = loss;
+  end.saved = saved;
+  c->stats = hoccl_stats_t{};
+  DeviceScope scope(c->device);
+  CU_TRY(c, scope.err);
+  if (grid) {
+    void* params[1] = {&a};
+    CU_TRY(c, launch_in_order_params(route_entry((int)f->dtype, shape, vec, false), (int)grid, kRouteThreads, params, (cudaStream_t)stream, 0,
+                                     (size_t)kRouteWarps * f->experts * sizeof(float)));
+  }
+  CU_TRY(c, launch_in_order(reinterpret_cast<const void*>(&route_end_kernel), kEndCtas, 1024, &end, (cudaStream_t)stream));
+  c->stats.host_launch_us = now_us() - t0;
+  return HOCCL_OK;
+}
+
+hoccl_result_t hoccl_route_backward(const void* const* logits, size_t ld, const size_t* tokens, const hoccl_route_config_t* f, const int32_t* const* indices,
+                                    const float* saved, const float* const* dweights, const float* dloss, void* const* dlogits, size_t dld, hoccl_comm_t c,
+                                    hoccl_stream_t stream) {
+  const double t0 = now_us();
+  hoccl_result_t rc = check_config(c, f, logits, ld, tokens);
+  if (rc != HOCCL_OK) return rc;
+  if ((dweights && !indices) || !saved || !dlogits || !aligned_to(saved, 4) || !aligned_to(dloss, 4) || dld < (size_t)f->experts || dld > 1ull << 31) return HOCCL_ERR_INVALID_ARG;
+  const size_t e = dtype_size((int)f->dtype);
+  const int shape = shape_of(f->experts), groups = f->per_rank ? c->R : 1;
+  RouteArgs a = {};
+  a.R = c->R;
+  a.experts = f->experts;
+  a.topk = f->topk;
+  a.groups = groups;
+  a.ld = ld;
+  a.dld = dld;
+  a.saved = saved;
+  a.dloss = dloss;
+  a.normalize = f->normalize;
+  bool vec = (f->experts * e) % 16 == 0 && (ld * e) % 16 == 0 && (dld * e) % 16 == 0;
+  try {
+    std::vector<Span> spans = {{(const char*)saved, (size_t)groups * (f->experts + 1) * 4, false}};
+    if (dloss) spans.push_back({(const char*)dloss, (size_t)groups * 4, false});
+    for (int r = 0; r < c->R; r++) {
+      if (!tokens[r]) continue;
+      if (!logits[r] || !dlogits[r] || !aligned_to(logits[r], e) || !aligned_to(dlogits[r], e)) return HOCCL_ERR_INVALID_ARG;
+      if (dweights && (!indices[r] || !dweights[r] || !aligned_to(indices[r], 4) || !aligned_to(dweights[r], 4))) return HOCCL_ERR_INVALID_ARG;
+      a.tokens[r] = (unsigned)tokens[r];
+      a.logits[r] = logits[r];
+      a.dlogits[r] = dlogits[r];
+      a.indices[r] = dweights ? const_cast<int32_t*>(indices[r]) : nullptr;
+      a.weights[r] = dweights ? const_cast<float*>(dweights[r]) : nullptr;
+      vec = vec && aligned_to(logits[r], 16) && aligned_to(dlogits[r], 16);
+      // in place: a row is read by the lanes that write it, before they do
+      if (!(dlogits[r] == logits[r] && dld == ld)) spans.push_back({(const char*)logits[r], rows_bytes(tokens[r], ld, f->experts, e), false});
+      spans.push_back({(const char*)dlogits[r], rows_bytes(tokens[r], dld, f->experts, e), true});
+      if (dweights) {
+        spans.push_back({(const char*)indices[r], tokens[r] * f->topk * 4, false});
+        spans.push_back({(const char*)dweights[r], tokens[r] * f->topk * 4, false});
+      }
+    }
+    if (spans_clash(&spans)) return HOCCL_ERR_INVALID_ARG;
+  } catch (const std::bad_alloc&) {
+    return HOCCL_ERR_INTERNAL;
+  }
+  c->stats = hoccl_stats_t{};
+  // an expert more or less costs the backward kernel no scratch: as many CTAs as two waves hold
+  const unsigned grid = share_rows(tokens, c->R, lanes_of(shape), 8 * kAllSms, &a.rows_per_cta, a.first);
+  if (!grid) return HOCCL_OK;
+  DeviceScope scope(c->device);
+  CU_TRY(c, scope.err);
+  CU_TRY(c, launch_in_order(route_entry((int)f->dtype, shape, vec, true), (int)grid, kRouteThreads, &a, (cudaStream_t)stream));
+  c->stats.host_launch_us = now_us() - t0;
+  return HOCCL_OK;
+}
+
+}  // extern "C"
