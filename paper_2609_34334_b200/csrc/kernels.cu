@@ -1018,15 +1018,14 @@ cudaError_t launch_in_order(const void* fn, int grid, int threads, void* args, c
   return launch_in_order_params(fn, grid, threads, params, stream, priority);
 }
 
-cudaError_t launch_in_order_params(const void* fn, int grid, int threads, void** params, cudaStream_t stream, int priority, size_t smem) {
+cudaError_t launch_in_order_params(const void* fn, int grid, int threads, void** params, cudaStream_t stream, int priority, int cluster) {
   cudaStreamCaptureStatus capture;
   const cudaError_t e = cudaStreamIsCapturing(stream, &capture);
   if (e != cudaSuccess) return e;
-  cudaLaunchAttribute attr[2];
+  cudaLaunchAttribute attr[3];
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cfg.attrs = attr;
   if (capture == cudaStreamCaptureStatusNone) {
@@ -1036,6 +1035,12 @@ cudaError_t launch_in_order_params(const void* fn, int grid, int threads, void**
   if (priority) {
     attr[cfg.numAttrs].id = cudaLaunchAttributePriority;
     attr[cfg.numAttrs++].val.priority = priority;
+  }
+  if (cluster > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = (unsigned)cluster;
+    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+    cfg.numAttrs++;
   }
   return cudaLaunchKernelExC(&cfg, fn, params);
 }

@@ -214,7 +214,7 @@ void prepare_ring_phase(RingSeg* seg, int nseg, int kind, int dtype, int threads
 // (wait_for_stream), so the order and what a kernel sees are those of a plain launch.  `fn` must be such a kernel.
 // Without the attribute while the stream is being captured: the capture keeps full edges.
 cudaError_t launch_in_order(const void* fn, int grid, int threads, void* args, cudaStream_t stream, int priority = 0);
-cudaError_t launch_in_order_params(const void* fn, int grid, int threads, void** params, cudaStream_t stream, int priority = 0, size_t smem = 0);   // several parameters
+cudaError_t launch_in_order_params(const void* fn, int grid, int threads, void** params, cudaStream_t stream, int priority = 0, int cluster = 1);   // several parameters; CTAs of a cluster
 // The kernels that the operators of a training step may launch (optim.cu, router.cu).
 void add_optim_kernels(std::vector<const void*>* fns);
 void add_router_kernels(std::vector<const void*>* fns);

@@ -21,7 +21,9 @@ namespace hoccl {
 namespace {
 
 constexpr int kMaxExperts = 1024, kMaxTopk = 32;
-constexpr int kRouteThreads = 256, kRouteWarps = kRouteThreads / 32;
+constexpr int kRouteThreads = 256, kRouteWarps = kRouteThreads / 32;   // of a CTA whose lanes hold up to 16 logits; half for 32
+template <int V>
+constexpr int kWarpsFor = V <= 16 ? kRouteWarps : kRouteWarps / 2;
 constexpr int kRouteCtas = 4 * kAllSms;          // CTAs of a forward launch besides one for each rank: bounds the scratch
 constexpr int kEndCtas = 8;                      // one cluster
 
@@ -49,19 +51,18 @@ struct RouteEndArgs {
   int* counts[kMaxRanks];
 };
 
-// A number as an unsigned word of the same order; +0 and -0 alike; NaN below everything.
-__device__ __forceinline__ unsigned order_key(float x) {
-  const unsigned b = __float_as_uint(x + 0.0f);
-  return x != x ? 0u : b ^ ((int)b < 0 ? 0xffffffffu : 0x80000000u);
-}
-__device__ __forceinline__ float from_order_key(unsigned k) { return __uint_as_float(k ^ ((int)k < 0 ? 0x80000000u : 0xffffffffu)); }
-constexpr unsigned kClosedKey = 0x007fffffu;   // of -infinity: such an expert is not chosen
-
+// Over the L lanes of a row; a NaN counts only where there is nothing else.
 template <int L>
 __device__ __forceinline__ float lanes_max(float x) {
+  if constexpr (L == 32) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+  } else {
 #pragma unroll
-  for (int d = L / 2; d; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-  return x;
+    for (int d = L / 2; d; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+    return x;
+  }
 }
 template <int L>
 __device__ __forceinline__ float lanes_sum(float x) {
@@ -69,25 +70,12 @@ __device__ __forceinline__ float lanes_sum(float x) {
   for (int d = L / 2; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
   return x;
 }
-template <int L>
-__device__ __forceinline__ unsigned lanes_max(unsigned x) {
-  if constexpr (L == 32) {
-    return __reduce_max_sync(0xffffffffu, x);
-  } else {
+template <int V>
+__device__ __forceinline__ float largest(const float* x) {
+  float m = x[0];
 #pragma unroll
-    for (int d = L / 2; d; d >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, d));
-    return x;
-  }
-}
-template <int L>
-__device__ __forceinline__ unsigned lanes_min(unsigned x) {
-  if constexpr (L == 32) {
-    return __reduce_min_sync(0xffffffffu, x);
-  } else {
-#pragma unroll
-    for (int d = L / 2; d; d >>= 1) x = min(x, __shfl_xor_sync(0xffffffffu, x, d));
-    return x;
-  }
+  for (int i = 1; i < V; i++) m = fmaxf(m, x[i]);
+  return m;
 }
 
 // Which expert lane `lane`'s i-th logit belongs to.  VEC (rows that are whole, aligned vectors): V consecutive ones; else spread for coalescing.
@@ -126,39 +114,33 @@ __device__ __forceinline__ void load_row(const void* base, unsigned long long at
   }
 }
 
-// x -> exp(x - top) / their sum; the logarithm of the sum of exp(x).  A row without a logit above -infinity: probabilities 0, NaN where
-// the logit is, logarithm 0.  top and inv: p of a logit y of this row is exp(y - top) * inv.
+// Row whose largest logit is `top`: x -> exp(x - top); inv = 1 / their sum; the logarithm of the sum of exp(logit).  A row without a logit above -infinity:
+// 0, NaN where the logit is, inv 1, logarithm 0 (top is set to 0).
 template <int V, int L>
-__device__ __forceinline__ void softmax_row(float* x, float* log_sum, float* top_out, float* inv_out) {
-  float top = x[0];
-#pragma unroll
-  for (int i = 1; i < V; i++) top = fmaxf(top, x[i]);
-  top = lanes_max<L>(top);
-  const bool open = top > -INFINITY;
-  if (!open) top = 0.0f;
+__device__ __forceinline__ void softmax_row(float* x, float* top, float* log_sum, float* inv) {
+  const bool open = *top > -INFINITY;
+  if (!open) *top = 0.0f;
   float sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < V; i++) sum += x[i] = __expf(x[i] - top);
+  for (int i = 0; i < V; i++) sum += x[i] = __expf(x[i] - *top);
   sum = lanes_sum<L>(sum);
-  const float inv = open ? 1.0f / sum : 1.0f;
-#pragma unroll
-  for (int i = 0; i < V; i++) x[i] *= inv;
-  *log_sum = open ? top + logf(sum) : 0.0f;
-  *top_out = top;
-  *inv_out = inv;
+  *inv = open ? 1.0f / sum : 1.0f;
+  *log_sum = open ? *top + logf(sum) : 0.0f;
 }
 
+// The topk largest of a row without a pass over it for each: the topk-th largest of the lanes' own largest logits is a bar that at least topk logits reach, and
+// few more do (a dozen for 8 of 256); those are collected and each counts the ones in front of it.  (One search of the whole row for each choice took
+// 1090 instructions a row of 256 and 50 us for 32,000 rows, most of it on the half-rate integer pipe.)
 template <int DT, int V, int L, bool VEC>
-__global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_constant__ RouteArgs a) {
-  constexpr int G = 32 / L, kRows = kRouteWarps * G;   // rows of a warp, of the CTA, at a time
+__global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_constant__ RouteArgs a) {
+  constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;   // rows of a warp, of the CTA, at a time
   constexpr int K = L * V < kMaxTopk ? L * V : kMaxTopk;
-  extern __shared__ float sums[];                      // [kRouteWarps][experts] at the end
+  __shared__ __align__(16) uint2 found[kRows][L * V];            // {bits of the logit, expert} of a row's candidates
   __shared__ int count[L * V + 1];
-  __shared__ unsigned chosen_key[kRows][K];
-  __shared__ int chosen[kRows][K];
-  __shared__ float squares[kRouteWarps];
+  __shared__ uint2 chosen[kRows][K];
+  __shared__ float squares[W];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % L, group = threadIdx.x % 32 / L, slot = warp * G + group;
-  for (int e = threadIdx.x; e <= a.experts; e += kRouteThreads) count[e] = 0;
+  for (int e = threadIdx.x; e <= a.experts; e += W * 32) count[e] = 0;
   int r = 0;
   while (blockIdx.x >= a.first[r + 1]) r++;
   const unsigned row0 = (blockIdx.x - a.first[r]) * a.rows_per_cta, row1 = min(a.tokens[r], row0 + a.rows_per_cta);
@@ -168,56 +150,66 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_const
   for (unsigned base = row0 + warp * G; base < row1; base += kRows) {
     const unsigned row = base + group;
     const bool real = row < row1;
-    float x[V], log_sum, top, inv;
+    float x[V], log_sum, inv;
     if (real) {
       load_row<DT, V, L, VEC>(a.logits[r], row * a.ld, a.experts, lane, x);
     } else {
 #pragma unroll
       for (int i = 0; i < V; i++) x[i] = -INFINITY;
     }
-    unsigned key[V];
-#pragma unroll
-    for (int i = 0; i < V; i++) key[i] = order_key(x[i]);
-    softmax_row<V, L>(x, &log_sum, &top, &inv);
-#pragma unroll
-    for (int i = 0; i < V; i++) p_sum[i] += x[i];
-    z_sum += log_sum * log_sum;
-    float sel_sum = 0.0f;
-    for (int k = 0; k < a.topk; k++) {
-      unsigned best = key[0];
-#pragma unroll
-      for (int i = 1; i < V; i++) best = max(best, key[i]);
-      best = lanes_max<L>(best);
-      int mine = -1;
-#pragma unroll
-      for (int i = V - 1; i >= 0; i--)
-        if (key[i] == best) mine = i;                  // the lowest of this lane's
-      const unsigned e = lanes_min<L>(mine >= 0 ? (unsigned)expert_of<V, L, VEC>(lane, mine) : 0xffffffffu);
-      const bool found = best > kClosedKey;
-#pragma unroll
-      for (int i = 0; i < V; i++)
-        if (found && (unsigned)expert_of<V, L, VEC>(lane, i) == e) key[i] = 0;
-      if (lane == 0) {
-        chosen_key[slot][k] = best;
-        chosen[slot][k] = found ? (int)e : -1;
-        if (found) atomicAdd(&count[e], 1);
-      }
-      if (found) sel_sum += __expf(from_order_key(best) - top);
+    float best = largest<V>(x), top = lanes_max<L>(best), bar = top;
+    for (int k = 1; k < a.topk; k++) {   // equal ones fall together: the bar only gets lower
+      if (best == bar) best = -INFINITY;
+      bar = lanes_max<L>(best);
     }
-    if (lane == 0 && chosen[slot][0] >= 0) atomicAdd(&count[a.experts], 1);
+    bar = fmaxf(bar, -3.402823466e38f);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+      const bool in = x[i] >= bar;
+      const unsigned all = __ballot_sync(0xffffffffu, in), mine = L == 32 ? all : all >> (group * L) & ((1u << (L & 31)) - 1);
+      if (in) found[slot][n + __popc(mine & ((1u << lane) - 1))] = make_uint2(__float_as_uint(x[i]), expert_of<V, L, VEC>(lane, i));
+      n += __popc(mine);
+    }
     __syncwarp();
+    softmax_row<V, L>(x, &top, &log_sum, &inv);
+#pragma unroll
+    for (int i = 0; i < V; i++) p_sum[i] += x[i] * inv;
+    z_sum += log_sum * log_sum;
+    for (int c = lane; c < n; c += L) {
+      const uint2 own = found[slot][c];
+      const float y = __uint_as_float(own.x);
+      int before = 0;
+      for (int j = 0; j < n; j++) {
+        const uint2 o = found[slot][j];
+        before += __uint_as_float(o.x) > y || (__uint_as_float(o.x) == y && o.y < own.y);
+      }
+      if (before < a.topk) {
+        chosen[slot][before] = own;
+        atomicAdd(&count[own.y], 1);
+      }
+    }
+    if (lane == 0 && n) atomicAdd(&count[a.experts], 1);
+    __syncwarp();
+    const int have = min(n, a.topk);
+    float part = 0.0f;
+    if (a.normalize) {
+      for (int k = lane; k < have; k += L) part += __expf(__uint_as_float(chosen[slot][k].x) - top);
+      part = lanes_sum<L>(part);
+    }
     if (real) {
-      const float scale = a.normalize ? 1.0f / sel_sum + 0.0f * inv : inv;   // a NaN in the row reaches its weights either way
+      const float scale = a.normalize ? 1.0f / part + 0.0f * inv : inv;   // a NaN in the row reaches its weights either way
       for (int k = lane; k < a.topk; k += L) {
-        const int e = chosen[slot][k];
         const unsigned long long at = (unsigned long long)row * a.topk + k;
-        a.indices[r][at] = e;
-        a.weights[r][at] = e < 0 ? 0.0f : __expf(from_order_key(chosen_key[slot][k]) - top) * scale;
+        a.indices[r][at] = k < have ? (int)chosen[slot][k].y : -1;
+        a.weights[r][at] = k < have ? __expf(__uint_as_float(chosen[slot][k].x) - top) * scale : 0.0f;
       }
     }
     __syncwarp();
   }
   // the CTA's sums: lanes of one expert, then warps, in order
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(found);   // [W][experts]
 #pragma unroll
   for (int i = 0; i < V; i++) {
 #pragma unroll
@@ -230,38 +222,45 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_const
   if (threadIdx.x % 32 == 0) squares[warp] = z_sum;
   __syncthreads();
   float* out = a.partial + (size_t)blockIdx.x * (2 * a.experts + 2);
-  for (int e = threadIdx.x; e < a.experts; e += kRouteThreads) {
+  for (int e = threadIdx.x; e < a.experts; e += W * 32) {
     float s = 0.0f;
-    for (int w = 0; w < kRouteWarps; w++) s += sums[w * a.experts + e];
+    for (int w = 0; w < W; w++) s += sums[w * a.experts + e];
     out[e] = s;
     out[a.experts + e] = __int_as_float(count[e]);
   }
   if (threadIdx.x == 0) {
     float z = 0.0f;
-    for (int w = 0; w < kRouteWarps; w++) z += squares[w];
+    for (int w = 0; w < W; w++) z += squares[w];
     out[2 * a.experts] = __int_as_float(count[a.experts]);
     out[2 * a.experts + 1] = z;
   }
 }
 
-// Adds the CTAs' sums.  One cluster; each CTA takes 32 experts at a time (a lane each, the warps share the forward CTAs), the first CTA
-// adds the parts of the loss.
-__global__ void __cluster_dims__(kEndCtas, 1, 1) __launch_bounds__(1024) route_end_kernel(const __grid_constant__ RouteEndArgs a) {
+// Adds the CTAs' sums.  One cluster of one or kEndCtas CTAs; a CTA takes 32 experts at a time, a lane each.  Its 32 warps share the ranks, and the forward CTAs
+// of a rank where there are fewer ranks than warps, so that all loads are in flight at once; the first CTA adds the parts of the loss.
+__global__ void __launch_bounds__(1024) route_end_kernel(const __grid_constant__ RouteEndArgs a) {
   namespace cg = cooperative_groups;
-  __shared__ double p_part[32][33];
-  __shared__ int c_part[32][33];
+  __shared__ float p_part[32][32];
+  __shared__ int c_part[32][32];
+  __shared__ double p_rank[kMaxRanks][32];
+  __shared__ int c_rank[kMaxRanks][32];
   __shared__ int rows[kMaxRanks];
   __shared__ double logs[kMaxRanks], loss[kMaxRanks];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   cg::cluster_group cluster = cg::this_cluster();
+  const int ctas = gridDim.x;
+  int split = 1;
+  while (split * 2 * a.R <= 32) split *= 2;      // warps of one rank
+  if (threadIdx.x < kMaxRanks) loss[threadIdx.x] = 0;
   wait_for_stream();
   const size_t words = 2 * (size_t)a.experts + 2;
-  for (int r = warp; r < a.R; r += 32) {   // every CTA needs the ranks' rows
+  for (int r = warp; r < a.R; r += 32) {         // every CTA needs the ranks' rows
     int n = 0;
     double z = 0;
     for (unsigned b = a.first[r] + lane; b < a.first[r + 1]; b += 32) {
-      n += __float_as_int(__ldcg(a.partial + b * words + 2 * a.experts));
-      z += __ldcg(a.partial + b * words + 2 * a.experts + 1);
+      const float2 end = make_float2(__ldcg(a.partial + b * words + 2 * a.experts), __ldcg(a.partial + b * words + 2 * a.experts + 1));
+      n += __float_as_int(end.x);
+      z += end.y;
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
@@ -273,74 +272,94 @@ __global__ void __cluster_dims__(kEndCtas, 1, 1) __launch_bounds__(1024) route_e
       logs[r] = z;
     }
   }
-  if (threadIdx.x < kMaxRanks) loss[threadIdx.x] = 0;
-  __syncthreads();
-  long long all = 0;
-  for (int r = 0; r < a.R; r++) all += rows[r];
-  for (int e0 = 32 * blockIdx.x; e0 < a.experts; e0 += 32 * kEndCtas) {
+  for (int e0 = 32 * blockIdx.x; e0 < a.experts; e0 += 32 * ctas) {
     const int e = e0 + lane;
-    double p_all = 0;
-    long long c_all = 0;
-    for (int r = 0; r < a.R; r++) {
-      double p = 0;
+    for (int r0 = 0; r0 < a.R; r0 += 32 / split) {
+      const int r = r0 + warp / split;
+      float p = 0;
       int n = 0;
-      if (e < a.experts)
-        for (unsigned b = a.first[r] + warp; b < a.first[r + 1]; b += 32) {
-          p += __ldcg(a.partial + b * words + e);
-          n += __float_as_int(__ldcg(a.partial + b * words + a.experts + e));
+      if (r < a.R && e < a.experts) {
+        const float* from = a.partial + e;
+#pragma unroll 4
+        for (unsigned b = a.first[r] + warp % split; b < a.first[r + 1]; b += split) {
+          p += __ldcg(from + b * words);
+          n += __float_as_int(__ldcg(from + b * words + a.experts));
         }
-      __syncthreads();
+      }
       p_part[warp][lane] = p;
       c_part[warp][lane] = n;
       __syncthreads();
-      if (warp == 0) {
-        p = 0;
+      if (warp % split == 0 && r < a.R) {
+        double sum = 0;
         n = 0;
-        for (int w = 0; w < 32; w++) {
-          p += p_part[w][lane];
-          n += c_part[w][lane];
+        for (int w = 0; w < split; w++) {
+          sum += p_part[warp + w][lane];
+          n += c_part[warp + w][lane];
         }
+        p_rank[r][lane] = sum;
+        c_rank[r][lane] = n;
         if (e < a.experts) a.counts[r][e] = n;
-        p_all += p;
-        c_all += n;
-        if (a.groups > 1 || r == a.R - 1) {   // a group ends here
-          const int g = a.groups > 1 ? r : 0;
-          const double rows_here = a.groups > 1 ? rows[r] : (double)all, f = rows_here > 0 ? c_all / (a.topk * rows_here) : 0;
-          if (e < a.experts) a.saved[(size_t)g * (a.experts + 1) + e] = (float)(rows_here > 0 ? a.balance * f / rows_here : 0);
-          double part = rows_here > 0 ? f * p_all / rows_here : p_all;   // no rows: 0, or NaN
-#pragma unroll
-          for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
-          if (lane == 0) loss[g] += part;
-          p_all = 0;
-          c_all = 0;
-        }
       }
+      __syncthreads();
     }
+    for (int g = warp; g < a.groups; g += 32) {
+      const int r0 = a.groups > 1 ? g : 0, r1 = a.groups > 1 ? g + 1 : a.R;
+      double p = 0;
+      long long c = 0, n = 0;
+      for (int r = r0; r < r1; r++) {
+        p += p_rank[r][lane];
+        c += c_rank[r][lane];
+        n += rows[r];
+      }
+      const double f = n ? (double)c / ((double)a.topk * n) : 0;
+      if (e < a.experts) a.saved[(size_t)g * (a.experts + 1) + e] = (float)(n ? a.balance * f / n : 0);
+      double part = n ? f * p / n : p;           // no rows: 0, or NaN
+#pragma unroll
+      for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
+      if (lane == 0) loss[g] += part;
+    }
+    __syncthreads();
   }
-  cluster.sync();
+  if (ctas > 1) cluster.sync();
+  else __syncthreads();
   if (blockIdx.x == 0) {
     for (int r = threadIdx.x; r < a.R; r += 1024) a.counts[r][a.experts] = rows[r];
     for (int g = threadIdx.x; g < a.groups; g += 1024) {
-      double n = a.groups > 1 ? rows[g] : (double)all, z = logs[g], l = 0;
-      if (a.groups == 1)
-        for (int r = 1; r < a.R; r++) z += logs[r];
-      for (int c = 0; c < kEndCtas; c++) l += *cluster.map_shared_rank(&loss[g], c);
+      const int r0 = a.groups > 1 ? g : 0, r1 = a.groups > 1 ? g + 1 : a.R;
+      double z = 0, l = 0;
+      long long n = 0;
+      for (int r = r0; r < r1; r++) {
+        z += logs[r];
+        n += rows[r];
+      }
+      for (int c = 0; c < ctas; c++) l += ctas > 1 ? *cluster.map_shared_rank(&loss[g], c) : loss[g];
       a.loss[2 * g] = (float)(a.balance * l);
-      a.loss[2 * g + 1] = (float)(n > 0 ? a.z * z / n : 0);
-      a.saved[(size_t)g * (a.experts + 1) + a.experts] = (float)(n > 0 ? 2 * a.z / n : 0);
+      a.loss[2 * g + 1] = (float)(n ? a.z * z / n : 0);
+      a.saved[(size_t)g * (a.experts + 1) + a.experts] = (float)(n ? 2 * a.z / n : 0);
     }
   }
-  cluster.sync();   // the others' shared memory lives until it has been read
+  if (ctas > 1) cluster.sync();                  // the others' shared memory lives until it has been read
 }
 
+template <int DT>
+__device__ __forceinline__ float logit_at(const void* base, unsigned long long at) {
+  return DT == 0 ? static_cast<const float*>(base)[at] : __uint_as_float((unsigned)static_cast<const unsigned short*>(base)[at] << 16);
+}
+
+// dlogits_j = p_j (c_j - shift) + what the weights' gradient adds to the chosen.  The latter comes through shared memory, where expert e of a row lies at
+// the place that its lane reads without a bank conflict; what was added is set back to zero behind the row.
 template <int DT, int V, int L, bool VEC>
-__global__ void __launch_bounds__(kRouteThreads) route_backward_kernel(const __grid_constant__ RouteArgs a) {
-  constexpr int G = 32 / L, kRows = kRouteWarps * G;
-  __shared__ float extra[kRows][L * V];   // by expert: what the weights' gradient adds
+__global__ void __launch_bounds__(kWarpsFor<V> * 32) route_backward_kernel(const __grid_constant__ RouteArgs a) {
+  constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;
+  __shared__ float extra[kRows][L * V];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % L, group = threadIdx.x % 32 / L, slot = warp * G + group;
+  const auto place = [](int e) { return VEC ? e % V * L + e / V : e; };
   int r = 0;
   while (blockIdx.x >= a.first[r + 1]) r++;
   const unsigned row0 = (blockIdx.x - a.first[r]) * a.rows_per_cta, row1 = min(a.tokens[r], row0 + a.rows_per_cta);
+  const bool with = a.weights[r] != nullptr, alone = a.topk <= L;   // a lane holds one of the chosen at most
+#pragma unroll
+  for (int i = 0; i < V; i++) extra[slot][i * L + lane] = 0.0f;
   wait_for_stream();
   const int g = a.groups > 1 ? r : 0;
   const float scale = a.dloss ? a.dloss[g] : 1.0f, z = a.saved[(size_t)g * (a.experts + 1) + a.experts] * scale;
@@ -353,61 +372,79 @@ __global__ void __launch_bounds__(kRouteThreads) route_backward_kernel(const __g
   for (unsigned base = row0 + warp * G; base < row1; base += kRows) {
     const unsigned row = base + group;
     const bool real = row < row1;
-    float x[V], log_sum, top, inv;
+    const unsigned long long logits_at = row * a.ld, chosen_at = (unsigned long long)row * a.topk;
+    // this lane's choice: expert, gradient of its weight, logit
+    int e = -1;
+    float dw = 0.0f, y = 0.0f;
+    if (with && alone && real && lane < a.topk) {
+      e = a.indices[r][chosen_at + lane];
+      dw = a.weights[r][chosen_at + lane];
+    }
+    float x[V], log_sum, inv;
     if (real) {
-      load_row<DT, V, L, VEC>(a.logits[r], row * a.ld, a.experts, lane, x);
+      load_row<DT, V, L, VEC>(a.logits[r], logits_at, a.experts, lane, x);
     } else {
 #pragma unroll
       for (int i = 0; i < V; i++) x[i] = -INFINITY;
     }
-    softmax_row<V, L>(x, &log_sum, &top, &inv);
+    const bool valid = (unsigned)e < (unsigned)a.experts;
+    if (valid) y = logit_at<DT>(a.logits[r], logits_at + e);
+    float top = lanes_max<L>(largest<V>(x));
+    softmax_row<V, L>(x, &top, &log_sum, &inv);
     float mean = 0.0f;   // of c under p
 #pragma unroll
-    for (int i = 0; i < V; i++) mean += x[i] * c[i];
+    for (int i = 0; i < V; i++) mean += (x[i] *= inv) * c[i];
     mean = lanes_sum<L>(mean);
     float shift = mean - z * log_sum;
-    if (a.weights[r] != nullptr) {
-#pragma unroll
-      for (int i = 0; i < V; i++) extra[slot][i * L + lane] = 0.0f;
-      __syncwarp();
-      // weights of the chosen and their gradients' mean
-      float w_sum = 0.0f, dw_sum = 0.0f;
-      for (int k = lane; k < a.topk && real; k += L) {
-        const unsigned long long at = (unsigned long long)row * a.topk + k;
-        const unsigned e = (unsigned)a.indices[r][at];
-        if (e < (unsigned)a.experts) {
-          const unsigned long long l = row * a.ld + e;
-          const float y = DT == 0 ? static_cast<const float*>(a.logits[r])[l] : __uint_as_float((unsigned)static_cast<const unsigned short*>(a.logits[r])[l] << 16);
-          const float p = __expf(y - top) * inv;
-          w_sum += p;
-          dw_sum += p * a.weights[r][at];
+    if (with) {
+      float w = 0.0f, dws = 0.0f;   // sums of p and of p * dw over this lane's choices
+      if (alone) {
+        w = valid ? __expf(y - top) * inv : 0.0f;
+        dws = valid ? w * dw : 0.0f;
+      } else {
+        for (int k = lane; k < a.topk && real; k += L) {
+          const unsigned i = (unsigned)a.indices[r][chosen_at + k];
+          if (i >= (unsigned)a.experts) continue;
+          const float p = __expf(logit_at<DT>(a.logits[r], logits_at + i) - top) * inv;
+          w += p;
+          dws += p * a.weights[r][chosen_at + k];
         }
       }
-      w_sum = lanes_sum<L>(w_sum);
-      dw_sum = lanes_sum<L>(dw_sum);
-      const float per = a.normalize ? (w_sum > 0.0f ? 1.0f / w_sum : w_sum) : 1.0f;
-      const float inner = dw_sum * per;
-      for (int k = 0; k < a.topk; k++) {   // one after the other: an index that comes twice adds twice
-        if (real && lane == k % L) {
-          const unsigned long long at = (unsigned long long)row * a.topk + k;
-          const unsigned e = (unsigned)a.indices[r][at];
-          if (e < (unsigned)a.experts) {
-            const unsigned long long l = row * a.ld + e;
-            const float y = DT == 0 ? static_cast<const float*>(a.logits[r])[l] : __uint_as_float((unsigned)static_cast<const unsigned short*>(a.logits[r])[l] << 16);
-            extra[slot][e] += __expf(y - top) * inv * per * (a.weights[r][at] - (a.normalize ? inner : 0.0f));
+      const float w_sum = lanes_sum<L>(w), dw_sum = lanes_sum<L>(dws);
+      const float per = a.normalize ? (w_sum > 0.0f ? 1.0f / w_sum : w_sum) : 1.0f;   // 0 or NaN stays
+      const float inner = dw_sum * per, less = a.normalize ? inner : 0.0f;
+      // an index that comes twice in a row adds twice, one after the other in the order of k
+      const unsigned same = alone ? __match_any_sync(0xffffffffu, valid ? group * kMaxExperts + e : -1 - (int)(threadIdx.x % 32)) : 0;
+      if (alone && !__any_sync(0xffffffffu, (same & (same - 1)) != 0)) {
+        if (valid) extra[slot][place(e)] = w * per * (dw - less);
+      } else {
+        for (int k = 0; k < a.topk; k++) {
+          if (real && lane == k % L) {
+            const unsigned i = (unsigned)a.indices[r][chosen_at + k];
+            if (i < (unsigned)a.experts)
+              extra[slot][place((int)i)] += __expf(logit_at<DT>(a.logits[r], logits_at + i) - top) * inv * per * (a.weights[r][chosen_at + k] - less);
           }
+          __syncwarp();
         }
-        __syncwarp();
       }
       if (!a.normalize) shift += inner;
+      __syncwarp();
+    }
+#pragma unroll
+    for (int i = 0; i < V; i++) x[i] *= c[i] - shift;
+    if (with) {
+#pragma unroll
+      for (int i = 0; i < V; i++) x[i] += extra[slot][i * L + lane];
+      __syncwarp();
+      if (alone) {
+        if (valid) extra[slot][place(e)] = 0.0f;
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; i++) extra[slot][i * L + lane] = 0.0f;
+      }
+      __syncwarp();
     }
     if (real) {
-      float d[V];
-#pragma unroll
-      for (int i = 0; i < V; i++) {
-        const int e = expert_of<V, L, VEC>(lane, i);
-        d[i] = x[i] * (c[i] - shift) + (a.weights[r] != nullptr ? extra[slot][e] : 0.0f);
-      }
       const unsigned long long at = row * a.dld;
       if (VEC) {
         constexpr int VE = Traits<DT>::VE;
@@ -415,28 +452,25 @@ __global__ void __launch_bounds__(kRouteThreads) route_backward_kernel(const __g
 #pragma unroll
         for (int j = 0; j < V / VE; j++)
           if (lane * V + j * VE < a.experts) {
-            uint4 o;
             unsigned w[4];
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-              if (DT == 0) w[i] = __float_as_uint(d[j * VE + i]);
-              else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(d[j * VE + 2 * i + 1]), "f"(d[j * VE + 2 * i]));
+              if (DT == 0) w[i] = __float_as_uint(x[j * VE + i]);
+              else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(x[j * VE + 2 * i + 1]), "f"(x[j * VE + 2 * i]));
             }
-            o = make_uint4(w[0], w[1], w[2], w[3]);
-            __stcs(p + lane * (V / VE) + j, o);
+            __stcs(p + lane * (V / VE) + j, make_uint4(w[0], w[1], w[2], w[3]));
           }
       } else {
 #pragma unroll
         for (int i = 0; i < V; i++) {
-          const int e = expert_of<V, L, VEC>(lane, i);
-          if (e < a.experts) {
-            if (DT == 0) static_cast<float*>(a.dlogits[r])[at + e] = d[i];
-            else static_cast<__nv_bfloat16*>(a.dlogits[r])[at + e] = __float2bfloat16_rn(d[i]);
+          const int to = expert_of<V, L, VEC>(lane, i);
+          if (to < a.experts) {
+            if (DT == 0) static_cast<float*>(a.dlogits[r])[at + to] = x[i];
+            else static_cast<__nv_bfloat16*>(a.dlogits[r])[at + to] = __float2bfloat16_rn(x[i]);
           }
         }
       }
     }
-    __syncwarp();
   }
 }
 
@@ -450,6 +484,8 @@ int shape_of(int experts) {
   return s;
 }
 int lanes_of(int shape) { return 1 << std::min(shape, 5); }
+int warps_of(int shape) { return shape == 7 ? kRouteWarps / 2 : kRouteWarps; }
+size_t rows_at_once(int shape) { return (size_t)warps_of(shape) * (32 / lanes_of(shape)); }
 
 template <int DT, bool VEC>
 const void* route_entry_of(int shape, bool backward) {
@@ -494,10 +530,10 @@ hoccl_result_t check_config(const hoccl_comm* c, const hoccl_route_config_t* f, 
 }
 
 // Rows of one CTA and the ranks' first CTAs: as many CTAs as `most` at most, besides one for each rank, and no fewer rows in one than its warps hold.
-unsigned share_rows(const size_t* tokens, int R, int lanes, unsigned most, unsigned* rows_per_cta, unsigned* first) {
+unsigned share_rows(const size_t* tokens, int R, int shape, unsigned most, unsigned* rows_per_cta, unsigned* first) {
   unsigned long long all = 0;
   for (int r = 0; r < R; r++) all += tokens[r];
-  const unsigned long long at_once = (unsigned long long)kRouteWarps * (32 / lanes);
+  const unsigned long long at_once = rows_at_once(shape);
   unsigned long long per = (all + most - 1) / most;
   per = std::max((per + at_once - 1) / at_once, 1ull) * at_once;
   *rows_per_cta = (unsigned)per;
@@ -521,7 +557,7 @@ extern "C" {
 
 size_t hoccl_route_scratch_bytes(int R, size_t max_tokens, int experts) {
   if (R < 1 || R > kMaxRanks || experts < 1 || experts > kMaxExperts) return 0;
-  const size_t at_once = (size_t)kRouteWarps * (32 / lanes_of(shape_of(experts)));
+  const size_t at_once = rows_at_once(shape_of(experts));
   const size_t ctas = std::min((size_t)R * ((max_tokens + at_once - 1) / at_once), (size_t)kRouteCtas + R);
   return (ctas * (2 * (size_t)experts + 2) * sizeof(float) + 255) / 256 * 256;
 }
@@ -565,7 +601,7 @@ hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* t
   } catch (const std::bad_alloc&) {
     return HOCCL_ERR_INTERNAL;
   }
-  const unsigned grid = share_rows(tokens, c->R, lanes_of(shape), kRouteCtas, &a.rows_per_cta, a.first);
+  const unsigned grid = share_rows(tokens, c->R, shape, kRouteCtas, &a.rows_per_cta, a.first);
   const size_t need = (size_t)grid * (2 * (size_t)f->experts + 2) * sizeof(float);
   if (need && (!c->scratch || c->scratch_bytes < need)) return HOCCL_ERR_SCRATCH;
   std::copy(a.first, a.first + kMaxRanks + 1, end.first);
@@ -579,11 +615,12 @@ hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* t
   DeviceScope scope(c->device);
   CU_TRY(c, scope.err);
   if (grid) {
-    void* params[1] = {&a};
-    CU_TRY(c, launch_in_order_params(route_entry((int)f->dtype, shape, vec, false), (int)grid, kRouteThreads, params, (cudaStream_t)stream, 0,
-                                     (size_t)kRouteWarps * f->experts * sizeof(float)));
+    CU_TRY(c, launch_in_order(route_entry((int)f->dtype, shape, vec, false), (int)grid, 32 * warps_of(shape), &a, (cudaStream_t)stream));
   }
-  CU_TRY(c, launch_in_order(reinterpret_cast<const void*>(&route_end_kernel), kEndCtas, 1024, &end, (cudaStream_t)stream));
+  // few sums are read by one CTA in less time than a cluster takes to start and meet
+  const int ctas = (size_t)grid * f->experts <= 16384 ? 1 : std::min(kEndCtas, (f->experts + 31) / 32);
+  void* params[1] = {&end};
+  CU_TRY(c, launch_in_order_params(reinterpret_cast<const void*>(&route_end_kernel), ctas, 1024, params, (cudaStream_t)stream, 0, ctas));
   c->stats.host_launch_us = now_us() - t0;
   return HOCCL_OK;
 }
@@ -635,11 +672,11 @@ hoccl_result_t hoccl_route_backward(const void* const* logits, size_t ld, const 
   }
   c->stats = hoccl_stats_t{};
   // an expert more or less costs the backward kernel no scratch: as many CTAs as two waves hold
-  const unsigned grid = share_rows(tokens, c->R, lanes_of(shape), 8 * kAllSms, &a.rows_per_cta, a.first);
+  const unsigned grid = share_rows(tokens, c->R, shape, 8 * kAllSms, &a.rows_per_cta, a.first);
   if (!grid) return HOCCL_OK;
   DeviceScope scope(c->device);
   CU_TRY(c, scope.err);
-  CU_TRY(c, launch_in_order(route_entry((int)f->dtype, shape, vec, true), (int)grid, kRouteThreads, &a, (cudaStream_t)stream));
+  CU_TRY(c, launch_in_order(route_entry((int)f->dtype, shape, vec, true), (int)grid, 32 * warps_of(shape), &a, (cudaStream_t)stream));
   c->stats.host_launch_us = now_us() - t0;
   return HOCCL_OK;
 }
