@@ -540,7 +540,7 @@ typedef struct {
 } hoccl_adamw_rates_t;
 
 typedef struct {
-  double lr, beta1, beta2, eps;  /* finite; 0 <= beta < 1; eps > 0 */
+  double lr, beta1, beta2, eps;  /* finite; 0 <= beta < 1; eps a positive normal binary32 number */
   double grad_scale;             /* the gradients are multiplied by it (1 / R for a mean over R ranks) */
   long step;                     /* 1 for the first */
   uint32_t seed;                 /* HOCCL_STATE_8BIT: of the rounding; another one each step */
@@ -554,14 +554,16 @@ typedef struct {
  *     g = s * grad;  m = beta1 * m + (1 - beta1) * g;  v = beta2 * v + (1 - beta2) * g^2
  *     p = p * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * with p = master, or param where there is none (a bf16 param without a master is rounded at every step, to nearest even).
+ * g, m, v and sqrt(v) are the binary32 results of these operations, each rounded by itself in the order (beta1 * m) + ((1 - beta1) * g) and
+ * (beta2 * v) + ((g * g) * (1 - beta2)), the constants rounded once; the weights may be a few units in the last place of their step off.
  * The weights are computed from m and v as they are before they are stored.  HOCCL_STATE_8BIT stores m and sqrt(v) with stochastic rounding:
- * u = value * (448 / largest of the block) becomes the e4m3 number below or above it, above with the probability of its distance from the one
+ * u = value * ((1 / largest of the block) * 448) becomes the e4m3 number below or above it, above with the probability of its distance from the one
  * below in units of 1/65536, so that an average that moves by less than a step of e4m3 (6 to 12 %) still moves; sqrt(v) > 0 never
  * becomes 0.  The random bits of element i (h = its tensor's number in the table, mix = the 32-bit finalizer of MurmurHash3):
  * w = mix(lo(i) + hi(i) * 632BE5AB + mix(seed + h * 9E3779B9)); m takes w mod 2^16, sqrt(v) takes w >> 16.  A block whose largest value is at most 1e-35
  * is stored as zeros.  A gradient that is not finite makes its element's weights and states NaN or infinite (8-bit states: of its block); a `factor` from hoccl_grad_norm
  * skips such a step.
- * Any alignment of a tensor to its element size is served; tensors whose arrays all start on 16-byte boundaries are faster.  Tensors and arrays must not
+ * Any alignment of a tensor to its element size is served; tensors whose arrays all start on 32-byte boundaries are faster.  Tensors and arrays must not
  * overlap, gradients excepted among themselves.  Either every tensor has a master or none; param_dtype must then be HOCCL_BFLOAT16.
  * hoccl_adamw_create errors: INVALID_ARG (NULL, n < 0, misaligned, overlapping, masters of some tensors only, weight_decay not finite),
  * UNSUPPORTED (dtype, state, a master beside fp32 weights), INTERNAL (out of host memory).

@@ -135,6 +135,11 @@ hoccl_result_t hoccl_kernel_preloaded(int kind, hoccl_dtype_t dtype, int nops, i
  * NaN with different payloads}.  Both must be 0.
  */
 hoccl_result_t hoccl_selftest_bf16_add(unsigned long long* counts, hoccl_stream_t stream);
+/*
+ * The same for the square root of the AdamW step: compares it with CUDA's correctly rounded __fsqrt_rn for every binary32 number from 2^-96 to 2^96
+ * (outside that range the step calls __fsqrt_rn itself).  counts: two zeroed 64-bit words in DEVICE memory; then {roots that differ, numbers}.
+ */
+hoccl_result_t hoccl_selftest_root(unsigned long long* counts, hoccl_stream_t stream);
 
 /* ---------------------------------------------------------------- self-tests ------------------- */
 

@@ -731,6 +731,11 @@ hoccl_result_t hoccl_selftest_bf16_add(unsigned long long* counts, hoccl_stream_
   return launch_bf16_add_selftest(counts, (cudaStream_t)stream) == cudaSuccess ? HOCCL_OK : HOCCL_ERR_CUDA;
 }
 
+hoccl_result_t hoccl_selftest_root(unsigned long long* counts, hoccl_stream_t stream) {
+  if (!counts) return HOCCL_ERR_INVALID_ARG;
+  return launch_root_selftest(counts, (cudaStream_t)stream) == cudaSuccess ? HOCCL_OK : HOCCL_ERR_CUDA;
+}
+
 static RGroup group_of_moves(int n, const uint64_t* src, const uint64_t* dst, const uint64_t* len) {
   RGroup g;
   g.kind = OP_MOVE;

@@ -217,6 +217,7 @@ cudaError_t launch_in_order(const void* fn, int grid, int threads, void* args, c
 cudaError_t launch_in_order_params(const void* fn, int grid, int threads, void** params, cudaStream_t stream, int priority = 0, int cluster = 1);   // several parameters; CTAs of a cluster
 // The kernels that the operators of a training step may launch (optim.cu, router.cu).
 void add_optim_kernels(std::vector<const void*>* fns);
+cudaError_t launch_root_selftest(unsigned long long* counts, cudaStream_t stream);   // see root_selftest_kernel
 void add_router_kernels(std::vector<const void*>* fns);
 
 // Enqueue helpers (return the CUDA error of the launch).

@@ -32,7 +32,7 @@ enum { W_FP32 = 0, W_BF16 = 1, W_MASTER = 2 };
 struct AdamScalars {
   float lr, step_size, root_scale;   // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
   float beta1, grad1, beta2, grad2;  // grad1 = 1 - beta1, grad2 = 1 - beta2, rounded once
-  float eps, grad_scale;
+  float eps, grad_scale, one;        // one = 1: see add2
   unsigned seed;
   const float* factor;
   const hoccl_adamw_rates_t* rates;
@@ -98,6 +98,54 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
   return d;
 }
 
+// Two binary32 operations in one instruction, each rounded by itself: the step is bound by the issue of instructions, not by the lanes.
+struct Two {
+  unsigned long long w;
+};
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.w) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ Two two(float a) { return two(a, a); }
+__device__ __forceinline__ void split(Two x, float* a) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a[0]), "=f"(a[1]) : "l"(x.w)); }
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.w) : "l"(a.w), "l"(b.w));
+  return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.w) : "l"(a.w), "l"(b.w), "l"(c.w));
+  return r;
+}
+
+// a + b: the compiler turns a product and a packed sum into one fused operation, however each is marked; times a 1 that it cannot see through it does not.
+__device__ __forceinline__ Two add2(Two a, Two b, float one) { return fma2(a, two(one), b); }
+
+// Square roots rounded to nearest, of numbers within kRootLow .. kRootHigh: an approximate reciprocal root, one step of Goldschmidt's iteration for the
+// root and half the reciprocal, and the remainder's correction (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000
+// processor", 1990).  hoccl_selftest_root compares every number of the range with __fsqrt_rn.
+constexpr float kRootLow = 0x1p-96f, kRootHigh = 0x1p96f;
+__device__ __forceinline__ Two root_in_range(Two x) {
+  float a[2], y[2];
+  split(x, a);
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y[0]) : "f"(a[0]));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y[1]) : "f"(a[1]));
+  const Two yy = two(y[0], y[1]);
+  Two g = mul2(x, yy), h = mul2(yy, two(-0.5f));
+  const Two r = fma2(g, h, two(0.5f));
+  g = fma2(g, r, g);
+  h = fma2(h, r, h);
+  return fma2(fma2(g, g, mul2(x, two(-1.0f))), h, g);
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 // Where a lane's eight elements lie in its block, and which of them exist.
 template <bool VEC>
 __device__ __forceinline__ unsigned element(int lane, int i) {
@@ -125,6 +173,24 @@ __device__ __forceinline__ void load_floats(const void* base, unsigned long long
     }
   }
 }
+// A lane's eight gradients: as vectors of 16 bytes where they can be, so that those of several ranks fit the registers.
+template <int DT, bool VEC>
+struct Raw {
+  float x[8];
+  __device__ __forceinline__ void load(const void* base, unsigned long long at, unsigned left, int lane) { load_floats<DT, VEC>(base, at, left, lane, x); }
+  __device__ __forceinline__ void widen(float* y) const {
+#pragma unroll
+    for (int i = 0; i < 8; i++) y[i] = x[i];
+  }
+};
+template <>
+struct Raw<1, true> {
+  uint4 r;
+  __device__ __forceinline__ void load(const void* base, unsigned long long at, unsigned, int lane) {
+    r = __ldcs(reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(base) + at) + lane);
+  }
+  __device__ __forceinline__ void widen(float* y) const { widen8(r, y); }
+};
 template <int DT, bool VEC>
 __device__ __forceinline__ void store_floats(void* base, unsigned long long at, unsigned left, int lane, const float* x) {
   if (DT == 0) {
@@ -179,41 +245,51 @@ __device__ __forceinline__ void load_codes(const void* base, unsigned long long 
 #pragma unroll
   for (int i = 0; i < 4; i++) {
     const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(pair[i], __NV_E4M3)));
-    x[2 * i] = f.x * scale;
-    x[2 * i + 1] = f.y * scale;
+    split(mul2(two(f.x, f.y), two(scale)), x + 2 * i);
   }
 }
 
-// One number on the grid of e4m3 (3 bits of mantissa from 2^-6 on, steps of 2^-9 below), rounded down or, with the chance of what is
-// cut off, up.  Adding 2^-6 to a number below 2^-6 puts it where binary32's own grid of 3 bits has those steps.  `rnd`: 16 random bits.
-__device__ __forceinline__ float round_e4m3(float u, unsigned rnd) {
-  const float a = fabsf(u), shift = a < 0.015625f ? 0.015625f : 0.0f;
-  const unsigned b = (__float_as_uint(a + shift) + (rnd << 4)) & 0xfff00000u;
-  return copysignf(__uint_as_float(b) - shift, u);
+// One number on the grid of e4m3 (3 bits of mantissa from 2^-6 on, steps of 2^-9 below), rounded towards zero or, with the chance of what is
+// cut off, away from it.  rnd: 16 random bits at bits 4 to 19, just below the mantissa's third bit.  Adding 2^-6 to a number below
+// 2^-6 puts it where binary32's own grid of 3 bits has those steps.
+__device__ __forceinline__ float round_normal(float u, unsigned rnd) { return __uint_as_float((__float_as_uint(u) + rnd) & 0xfff00000u); }
+__device__ __forceinline__ float round_any(float u, unsigned rnd) {
+  const float shift = fabsf(u) < 0.015625f ? copysignf(0.015625f, u) : 0.0f;
+  return copysignf(round_normal(u + shift, rnd) - shift, u);
 }
-
-// Stores a block (x >= 0 for the root) and its scale.  The whole warp takes part.
+// Stores a block (x >= 0 for the root) and its scale.  The whole warp takes part.  A block without a number below 2^-6 of the codes' range, the usual
+// one, does without the steps for those: 4 instructions a number instead of 9.
 template <bool VEC, bool ROOT>
 __device__ __forceinline__ void store_codes(void* base, float* scales, unsigned long long at, unsigned left, int lane, const float* x, const unsigned* word) {
-  unsigned top_bits = 0;
+  float top = fabsf(x[0]), low = top;
 #pragma unroll
-  for (int i = 0; i < 8; i++) top_bits = max(top_bits, __float_as_uint(x[i]) & 0x7fffffffu);   // NaN is the largest
-  const float top = __uint_as_float(__reduce_max_sync(0xffffffffu, top_bits));
+  for (int i = 1; i < 8; i++) {
+    top = max_nan(top, fabsf(x[i]));
+    low = fminf(low, fabsf(x[i]));
+  }
+  top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));   // of non-negative numbers and NaN the words have their order
   const bool some = top > 1e-35f;
-  const float inv = some ? 448.0f / top : 0.0f;
+  const float inv = some ? __frcp_rn(top) * 448.0f : 0.0f;
   if (lane == 0) scales[at / kBlock] = some ? top * (1.0f / 448.0f) : top == top ? 0.0f : top;
+  float q[8];
+  if (__any_sync(0xffffffffu, low * inv < 0.015625f)) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const float u = x[i] * inv;
+      q[i] = round_any(u, ROOT ? word[i] >> 12 & 0xffff0u : word[i] << 4 & 0xffff0u);
+      if (ROOT && u > 0.0f) q[i] = fmaxf(q[i], 0.001953125f);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      split(mul2(two(x[i], x[i + 1]), two(inv)), q + i);
+#pragma unroll
+      for (int j = i; j < i + 2; j++) q[j] = round_normal(q[j], ROOT ? word[j] >> 12 & 0xffff0u : word[j] << 4 & 0xffff0u);
+    }
+  }
   unsigned short pair[4];
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    float q[2];
-#pragma unroll
-    for (int j = 0; j < 2; j++) {
-      const float u = x[2 * i + j] * inv;
-      q[j] = round_e4m3(u, ROOT ? word[2 * i + j] >> 16 : word[2 * i + j] & 0xffffu);
-      if (ROOT && u > 0.0f) q[j] = fmaxf(q[j], 0.001953125f);
-    }
-    pair[i] = __nv_cvt_float2_to_fp8x2(make_float2(q[0], q[1]), __NV_SATFINITE, __NV_E4M3);
-  }
+  for (int i = 0; i < 4; i++) pair[i] = __nv_cvt_float2_to_fp8x2(make_float2(q[2 * i], q[2 * i + 1]), __NV_SATFINITE, __NV_E4M3);
   unsigned char* p = static_cast<unsigned char*>(base) + at;
   if (VEC) {
     __stcs(reinterpret_cast<uint2*>(p) + lane, make_uint2(pair[0] | (unsigned)pair[1] << 16, pair[2] | (unsigned)pair[3] << 16));
@@ -248,12 +324,6 @@ __device__ __forceinline__ Rates read_rates(const AdamScalars& s) {
   return r;
 }
 
-__device__ __forceinline__ float sqrt_fast(float x) {   // off by at most 2^-23 of the root
-  float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
 // What a block's state and weight need besides its gradient.
 template <int W, int STATE, bool VEC>
 struct Held {
@@ -274,14 +344,33 @@ struct Held {
   // g: the gradients as they were read.  Afterwards p holds the new weights, which the caller stores; the state is stored here.
   __device__ __forceinline__ void step(const float* g, const AdamScalars& s, const Rates& r, float keep, unsigned key, float* master, void* mp, void* vp,
                                        float* ms, float* vs, unsigned long long at, unsigned left, int lane) {
+    // states: every operation rounded by itself, as the header has it, so that 8-bit codes can be told bit for bit
     float root[8];
+    float low = 3.4e38f, high = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const float x = g[i] * r.scale;
-      m[i] = s.beta1 * m[i] + s.grad1 * x;
-      v[i] = s.beta2 * (STATE == HOCCL_STATE_8BIT ? v[i] * v[i] : v[i]) + s.grad2 * (x * x);
-      root[i] = sqrt_fast(v[i]);
-      p[i] = p[i] * keep - r.step_size * __fdividef(m[i], root[i] * r.root_scale + s.eps);
+    for (int i = 0; i < 8; i += 2) {
+      const Two x = mul2(two(g[i], g[i + 1]), two(r.scale));
+      Two vv = two(v[i], v[i + 1]);
+      if (STATE == HOCCL_STATE_8BIT) vv = mul2(vv, vv);
+      split(add2(mul2(two(m[i], m[i + 1]), two(s.beta1)), mul2(x, two(s.grad1)), s.one), m + i);
+      split(add2(mul2(vv, two(s.beta2)), mul2(mul2(x, x), two(s.grad2)), s.one), v + i);
+      low = fminf(low, fminf(v[i], v[i + 1]));
+      high = max_nan(high, max_nan(v[i], v[i + 1]));
+    }
+    if (!__any_sync(0xffffffffu, !(low >= kRootLow && high <= kRootHigh))) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) split(root_in_range(two(v[i], v[i + 1])), root + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) root[i] = __fsqrt_rn(v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      float below[2], over[2];
+      split(fma2(two(root[i], root[i + 1]), two(r.root_scale), two(s.eps)), below);
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(over[0]) : "f"(below[0]));   // eps is a normal number
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(over[1]) : "f"(below[1]));
+      split(fma2(mul2(two(m[i], m[i + 1]), two(over[0], over[1])), two(-r.step_size), mul2(two(p[i], p[i + 1]), two(keep))), p + i);
     }
     if (W == W_MASTER) store_floats<0, VEC>(master, at, left, lane, p);
     if (STATE == HOCCL_STATE_FLOAT32) {
@@ -311,7 +400,7 @@ __device__ __forceinline__ void tensor_block(const AdamRow& t, const AdamScalars
 }
 
 template <int GT, int W, int STATE, class Table>
-__global__ void __launch_bounds__(kOptThreads) adamw_kernel(const __grid_constant__ Table t, const __grid_constant__ AdamScalars s) {
+__global__ void __launch_bounds__(kOptThreads, 4) adamw_kernel(const __grid_constant__ Table t, const __grid_constant__ AdamScalars s) {
   wait_for_stream();
   const Rates r = read_rates(s);
   if (r.skip) return;
@@ -336,33 +425,36 @@ __device__ __forceinline__ void sharded_block(const ShardedArgs& a, const AdamSc
                                               unsigned long long n, int lane) {
   const unsigned long long at = (unsigned long long)block * kBlock;
   const unsigned left = (unsigned)min(n - at, (unsigned long long)kBlock);
-  Held<W, STATE, VEC> h;
-  h.load(a.param[c], a.master[c], a.m[c], a.v[c], a.m_scale[c], a.v_scale[c], lo + at, at, left, lane);
-  // the ring's order: c + 1, c + 2, ..., c; four ranks' gradients in flight at a time
+  // the ring's order: c + 1, c + 2, ..., c; the gradients of kFlight ranks in flight at a time, as they lie in memory
+  constexpr int kFlight = !VEC ? 2 : GT == 1 ? 8 : 4;
   float g[8];
-  for (int j0 = 0; j0 < a.R; j0 += 4) {
-    float x[4][8];
+  int from = c;
+  for (int j0 = 0; j0 < a.R; j0 += kFlight) {
+    Raw<GT, VEC> x[kFlight];
 #pragma unroll
-    for (int j = 0; j < 4; j++)
+    for (int j = 0; j < kFlight; j++)
       if (j0 + j < a.R) {
-        int from = c + 1 + j0 + j;
-        from -= from >= a.R ? a.R : 0;
-        load_floats<GT, VEC>(a.grad[from], lo + at, left, lane, x[j]);
+        from = from + 1 < a.R ? from + 1 : 0;
+        x[j].load(a.grad[from], lo + at, left, lane);
       }
 #pragma unroll
-    for (int j = 0; j < 4; j++)
+    for (int j = 0; j < kFlight; j++)
       if (j0 + j < a.R) {
+        float y[8];
+        x[j].widen(y);
 #pragma unroll
-        for (int i = 0; i < 8; i++) g[i] = j0 + j ? __fadd_rn(g[i], x[j][i]) : x[j][i];
+        for (int i = 0; i < 8; i++) g[i] = j0 + j ? __fadd_rn(g[i], y[i]) : y[i];
       }
   }
+  Held<W, STATE, VEC> h;
+  h.load(a.param[c], a.master[c], a.m[c], a.v[c], a.m_scale[c], a.v_scale[c], lo + at, at, left, lane);
   h.step(g, s, r, fmaf(-r.lr, a.decay, 1.0f), STATE == HOCCL_STATE_8BIT ? tensor_key(r.seed, (unsigned)c) : 0, a.master[c], a.m[c], a.v[c], a.m_scale[c],
          a.v_scale[c], at, left, lane);
   for (int to = 0; to < a.R; to++) store_floats<W == W_FP32 ? 0 : 1, VEC>(a.param[to], lo + at, left, lane, h.p);
 }
 
 template <int GT, int W, int STATE>
-__global__ void __launch_bounds__(kOptThreads) sharded_adamw_kernel(const __grid_constant__ ShardedArgs a, const __grid_constant__ AdamScalars s) {
+__global__ void __launch_bounds__(kOptThreads, 2) sharded_adamw_kernel(const __grid_constant__ ShardedArgs a, const __grid_constant__ AdamScalars s) {
   wait_for_stream();
   const Rates r = read_rates(s);
   if (r.skip) return;
@@ -479,6 +571,21 @@ __global__ void __launch_bounds__(kNormThreads) norm_end_kernel(const __grid_con
   }
 }
 
+// Every number of kRootLow .. kRootHigh: counts[0] += roots that differ from __fsqrt_rn's, counts[1] += numbers.
+__global__ void __launch_bounds__(256) root_selftest_kernel(unsigned long long* counts) {
+  const unsigned lo = __float_as_uint(kRootLow), hi = __float_as_uint(kRootHigh);
+  unsigned long long wrong = 0, seen = 0;
+  for (unsigned b = lo + blockIdx.x * 256 + threadIdx.x; b <= hi; b += gridDim.x * 256) {
+    float r[2];
+    split(root_in_range(two(__uint_as_float(b), __uint_as_float(hi - (b - lo)))), r);
+    wrong += __float_as_uint(r[0]) != __float_as_uint(__fsqrt_rn(__uint_as_float(b)));
+    wrong += __float_as_uint(r[1]) != __float_as_uint(__fsqrt_rn(__uint_as_float(hi - (b - lo))));
+    seen++;
+  }
+  atomicAdd(counts, wrong);
+  atomicAdd(counts + 1, seen);
+}
+
 // ---------------------------------------------------------------- host: dispatch
 
 template <class Table>
@@ -522,10 +629,11 @@ bool fill_scalars(const hoccl_adamw_config_t& c, AdamScalars* s) {
   s->grad2 = (float)(1.0 - c.beta2);
   s->eps = (float)c.eps;
   s->grad_scale = (float)c.grad_scale;
+  s->one = 1.0f;
   s->seed = c.seed;
   s->factor = c.factor;
   s->rates = c.rates;
-  return s->eps > 0;
+  return s->eps >= 1.17549435e-38f;   // the kernels divide by numbers from eps on with a reciprocal that takes normal ones
 }
 
 struct Region {
@@ -564,6 +672,11 @@ bool state_fits(const void* m, const void* v, const float* master, const float* 
 }
 
 }  // namespace
+
+cudaError_t launch_root_selftest(unsigned long long* counts, cudaStream_t stream) {
+  root_selftest_kernel<<<8 * kAllSms, 256, 0, stream>>>(counts);
+  return cudaGetLastError();
+}
 
 void add_optim_kernels(std::vector<const void*>* fns) {
   for (int gt = 0; gt < 2; gt++) {

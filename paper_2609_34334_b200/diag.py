@@ -21,7 +21,7 @@ EXPORTS = [   # every function include/hoccl_diag.h declares
     "hoccl_options_resolve", "hoccl_plan_build", "hoccl_plan_destroy", "hoccl_plan_get_op",
     "hoccl_plan_group_deps", "hoccl_plan_inbox_slots", "hoccl_plan_num_groups", "hoccl_plan_num_ops",
     "hoccl_plan_scratch_bytes", "hoccl_plan_slot_bytes", "hoccl_port_probe", "hoccl_probe_copy_routes",
-    "hoccl_probe_move_needs_sm", "hoccl_selftest_barrier_timeout", "hoccl_selftest_roles_timeout", "hoccl_selftest_bf16_add", "hoccl_sum_launch",
+    "hoccl_probe_move_needs_sm", "hoccl_selftest_barrier_timeout", "hoccl_selftest_roles_timeout", "hoccl_selftest_bf16_add", "hoccl_selftest_root", "hoccl_sum_launch",
 ]
 
 
@@ -82,6 +82,7 @@ def lib() -> ctypes.CDLL:
         "hoccl_copy_launch": (i, [vp, vp, sz, i, vp]),
         "hoccl_fanout_launch": (i, [vp, vp, i, sz, i, vp]),
         "hoccl_selftest_bf16_add": (i, [vp, vp]),
+        "hoccl_selftest_root": (i, [vp, vp]),
         "hoccl_chain_launch": (i, [vp, sz, i, vp, vp, sz, i, i, vp]),
         "hoccl_fanout_inspect": (i, [i, vp, vp, vp, i, i, vp, vp, vp, vp, vp, vp, vp, ctypes.POINTER(i), ctypes.POINTER(i)]),
         "hoccl_move_inspect": (i, [i, vp, vp, vp, i, i, i, ctypes.POINTER(MoveSeg), vp, ctypes.POINTER(i)]),
@@ -184,6 +185,11 @@ def chain_launch(first, stride_bytes, nsrc, local, out, count, dtype, ctas, stre
 def selftest_bf16_add(counts, stream=None) -> int:
     """hoccl_selftest_bf16_add: counts = device array of two zeroed 64-bit words.  Returns the result code."""
     return lib().hoccl_selftest_bf16_add(_ptr(counts), _stream(stream))
+
+
+def selftest_root(counts, stream=None) -> int:
+    """hoccl_selftest_root: counts = device array of two zeroed 64-bit words.  Returns the result code."""
+    return lib().hoccl_selftest_root(_ptr(counts), _stream(stream))
 
 
 def fanout_inspect(moves, ctas: int = 8):

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2609_34334_b200 import binding as hb
+from paper_2609_34334_b200 import diag as hd
 from train_ref import BLOCK, DT, HALF, adamw, check_codes, decode, words
 
 pytestmark = pytest.mark.gpu
@@ -114,6 +115,67 @@ def test_formula(comm, param, master, grad, state, gap):
     factor = torch.tensor([0.5], device="cuda")
     comm.adamw(s.table(decay), 1e-3, 7, beta1=B1, beta2=B2, eps=EPS, grad_scale=0.25, factor=factor, seed=99)
     s.check(s.now(), 1e-3, 7, decay, 0.125, 99)
+
+
+def test_root_equals_the_correctly_rounded_one_for_every_number():
+    counts = torch.zeros(2, dtype=torch.int64, device="cuda")
+    torch.cuda.synchronize()
+    assert hd.selftest_root(counts) == hb.OK
+    torch.cuda.synchronize()
+    assert counts.tolist() == [0, 192 * 2 ** 23 + 1]
+
+
+def bits_of_a_step(p, g, m, v, ms, vs, scale, seed, tensor):
+    """The states of a step in numpy's binary32, operation by operation as the header has them: (m, v) or (codes, scales of m, of the root)."""
+    f = np.float32
+    x = g * f(scale)
+    if ms is not None:
+        m, v = (c * s for c, s in ((m, ms), (v, vs)))
+        v = v * v
+    m = m * f(B1) + x * f(1 - B1)
+    v = v * f(B2) + (x * x) * f(1 - B2)
+    if ms is None:
+        return m, v
+    w = words(seed, tensor, len(g)).numpy()
+    out = []
+    for y, rnd, root in ((m, w & 0xFFFF, False), (np.sqrt(v), w >> 16, True)):
+        full = np.zeros(-(-len(y) // BLOCK) * BLOCK, f)
+        full[:len(y)] = y
+        top = np.abs(full.reshape(-1, BLOCK)).max(1)
+        some = top > f(1e-35)
+        with np.errstate(divide="ignore", over="ignore", invalid="ignore"):
+            inv = np.where(some, (f(1) / top) * f(448), f(0)).astype(f)
+        u = y * np.repeat(inv, BLOCK)[:len(y)]
+        small = np.abs(u) < f(2.0 ** -6)
+        shift = np.where(small, f(2.0 ** -6), f(0))
+        b = (np.abs(u) + shift).astype(f).view(np.uint32) + (rnd.astype(np.uint32) << np.uint32(4)) & np.uint32(0xFFF00000)
+        q = b.view(f) - shift
+        if root:
+            q = np.where((u > 0) & (q == 0), f(2.0 ** -9), q)
+        out += [np.copysign(q, u), np.where(some, top * f(1 / 448), f(0)).astype(f)]
+    return out
+
+
+@pytest.mark.parametrize("state", ["fp32", "8bit"])
+@pytest.mark.parametrize("gap", [0, 3])
+@pytest.mark.parametrize("zeros", [0.0, 0.5])
+def test_states_bit_for_bit(comm, state, gap, zeros):
+    s = Set([257, 65_536, 5000], "bf16", False, "bf16", state, gap, seed=11)
+    if zeros:   # numbers in the codes' lowest range, roots outside the fast one
+        for k in "gmv":
+            hit = torch.rand(s.total, generator=torch.Generator().manual_seed(3)) < zeros
+            s.cpu[k] = torch.where(hit, torch.zeros_like(s.cpu[k].float()), s.cpu[k].float() * torch.logspace(-8, 0, s.total)).to(s.cpu[k].dtype)
+            s.dev[k].copy_(s.cpu[k])
+    comm.adamw(s.table(), 1e-3, 3, beta1=B1, beta2=B2, grad_scale=0.3, seed=77)
+    got = s.now()
+    for k, n in enumerate(s.counts):
+        a = lambda name, src: s.views(name, src)[k].float().numpy()  # noqa: E731
+        rep = lambda name: np.repeat(a(name, s.cpu), BLOCK)[:n] if state == "8bit" else None  # noqa: E731
+        want = bits_of_a_step(None, a("g", s.cpu), a("m", s.cpu), a("v", s.cpu), rep("ms"), rep("vs"), 0.3, 77, k)
+        names = ("m", "v") if state == "fp32" else ("m", "ms", "v", "vs")
+        for name, w in zip(names, want):
+            have = a(name, got)
+            assert np.array_equal(have, w), (name, k, np.flatnonzero(have != w)[:5], have[have != w][:5], w[have != w][:5])
 
 
 @pytest.mark.parametrize("state", ["fp32", "8bit"])
