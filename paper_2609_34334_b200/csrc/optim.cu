@@ -6,11 +6,14 @@
 // The unit of work is a block of 256 elements, one warp's: the elements that share a scale in 8-bit states, so that a block's
 // largest value is one warp reduction and states of either kind have one shape.  In an aligned, whole block lane l holds elements 8 l .. 8 l + 7 (32-byte
 // accesses of binary32 arrays, 16 of bf16, 8 of codes); in any other one elements l, l + 32, ...  Both run the same arithmetic: alignment changes no bit.
+// A CTA's warps take the blocks of one tile of one tensor, so that which tensor, and where in its arrays, is the same for the whole CTA: addresses are a
+// uniform base and the thread's own constant offset (found by each warp for itself they were a third of the instructions of a step with 8-bit states).
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 #include <new>
 #include <vector>
 
@@ -23,16 +26,21 @@ namespace hoccl {
 namespace {
 
 constexpr int kBlock = HOCCL_STATE_BLOCK;
-constexpr int kWarps = 8, kOptThreads = 32 * kWarps;
+constexpr int kWarps = 4, kOptThreads = 32 * kWarps, kTile = kWarps * kBlock;
 static_assert(kBlock == 256, "a warp holds a block with 8 elements a lane");
 
 // weights: binary32; bf16; bf16 beside a binary32 master
 enum { W_FP32 = 0, W_BF16 = 1, W_MASTER = 2 };
 
+// Twice the same number, as an operand of two operations at once: in the kernel's parameters it takes neither registers nor moves.
+struct Pair {
+  unsigned long long w;
+};
 struct AdamScalars {
+  Pair beta1, grad1, beta2, grad2;   // grad1 = 1 - beta1, grad2 = 1 - beta2, rounded once
+  Pair eps, one, half, minus_half, minus_one;   // one: see add2
   float lr, step_size, root_scale;   // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
-  float beta1, grad1, beta2, grad2;  // grad1 = 1 - beta1, grad2 = 1 - beta2, rounded once
-  float eps, grad_scale, one;        // one = 1: see add2
+  float grad_scale;
   unsigned seed;
   const float* factor;
   const hoccl_adamw_rates_t* rates;
@@ -46,22 +54,22 @@ struct AdamRow {
   float decay;
   unsigned flags;   // bit 0: aligned; the rest: number of the tensor in the caller's table
 };
-// Tensors by value: a launch carries up to 32 (2.4 KB of parameters) or up to 420 (32 KB, the most there is).
+// Tensors by value: a launch carries up to 32 (2.4 KB of parameters, 1.2 us of the host's time), 96 (7 KB) or 420 (32 KB, the most there is: 12 us).
 template <int N>
 struct AdamTableT {
-  unsigned blocks, per_warp;    // blocks of all tensors; of one warp
   int n, pad;
   AdamRow row[N];
-  unsigned first[N + 1];        // prefix sums of blocks
+  unsigned first[N + 1];        // prefix sums of tiles: a CTA each
 };
 using AdamTableSmall = AdamTableT<32>;
+using AdamTableMiddle = AdamTableT<96>;
 using AdamTable = AdamTableT<420>;
 static_assert(sizeof(AdamTable) + sizeof(AdamScalars) <= 32764, "kernel parameters");
 
 struct ShardedArgs {
   int R;
   float decay;
-  unsigned per_rank, per_warp;   // blocks of a full chunk; of one warp
+  unsigned per_rank;             // tiles of a full chunk: a CTA each
   unsigned long long count, q;
   unsigned long long aligned;    // bit c: chunk c
   const void* grad[kMaxRanks];
@@ -108,6 +116,7 @@ __device__ __forceinline__ Two two(float a, float b) {
   return r;
 }
 __device__ __forceinline__ Two two(float a) { return two(a, a); }
+__device__ __forceinline__ Two two(Pair a) { return Two{a.w}; }
 __device__ __forceinline__ void split(Two x, float* a) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a[0]), "=f"(a[1]) : "l"(x.w)); }
 __device__ __forceinline__ Two mul2(Two a, Two b) {
   Two r;
@@ -121,23 +130,23 @@ __device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
 }
 
 // a + b: the compiler turns a product and a packed sum into one fused operation, however each is marked; times a 1 that it cannot see through it does not.
-__device__ __forceinline__ Two add2(Two a, Two b, float one) { return fma2(a, two(one), b); }
+__device__ __forceinline__ Two add2(Two a, Two b, Pair one) { return fma2(a, two(one), b); }
 
 // Square roots rounded to nearest, of numbers within kRootLow .. kRootHigh: an approximate reciprocal root, one step of Goldschmidt's iteration for the
 // root and half the reciprocal, and the remainder's correction (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000
 // processor", 1990).  hoccl_selftest_root compares every number of the range with __fsqrt_rn.
 constexpr float kRootLow = 0x1p-96f, kRootHigh = 0x1p96f;
-__device__ __forceinline__ Two root_in_range(Two x) {
+__device__ __forceinline__ Two root_in_range(Two x, Two half, Two minus_half, Two minus_one) {
   float a[2], y[2];
   split(x, a);
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y[0]) : "f"(a[0]));
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y[1]) : "f"(a[1]));
   const Two yy = two(y[0], y[1]);
-  Two g = mul2(x, yy), h = mul2(yy, two(-0.5f));
-  const Two r = fma2(g, h, two(0.5f));
+  Two g = mul2(x, yy), h = mul2(yy, minus_half);
+  const Two r = fma2(g, h, half);
   g = fma2(g, r, g);
   h = fma2(h, r, h);
-  return fma2(fma2(g, g, mul2(x, two(-1.0f))), h, g);
+  return fma2(fma2(g, g, mul2(x, minus_one)), h, g);
 }
 
 __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
@@ -146,91 +155,109 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either 
   return r;
 }
 
-// Where a lane's eight elements lie in its block, and which of them exist.
-template <bool VEC>
-__device__ __forceinline__ unsigned element(int lane, int i) {
-  return VEC ? lane * 8 + i : i * 32 + lane;
+// How a block is read and written: element by element within the array's end, element by element all of it, or in aligned vectors.
+enum Mode { ENDS, WHOLE, VECTORS };
+// Where a thread's eight elements lie in its tile, and whether they exist where `left` elements do.
+template <Mode MODE>
+__device__ __forceinline__ unsigned element(int i) {
+  return MODE == VECTORS ? threadIdx.x * 8 + i : (threadIdx.x & ~31u) * 8 + i * 32 + (threadIdx.x & 31);
+}
+template <Mode MODE>
+__device__ __forceinline__ bool exists(int i, unsigned left) {
+  return MODE != ENDS || element<MODE>(i) < left;
 }
 
-// DT 0 binary32, 1 bf16.  `left`: elements of the array from the block's start (VEC: at least 256).
-template <int DT, bool VEC>
-__device__ __forceinline__ void load_floats(const void* base, unsigned long long at, unsigned left, int lane, float* x) {
+// DT 0 binary32, 1 bf16.  base: the tile's first element; `left`: elements of the array from there on (a block that is not ENDS lies within them).
+template <int DT, Mode MODE>
+__device__ __forceinline__ void load_floats(const void* base, unsigned left, float* x) {
   if (DT == 0) {
-    const float* p = static_cast<const float*>(base) + at;
-    if (VEC) {
-      load8(p + lane * 8, x);
+    const float* p = static_cast<const float*>(base);
+    if (MODE == VECTORS) {
+      load8(p + threadIdx.x * 8, x);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; i++) x[i] = i * 32 + lane < left ? __ldcs(p + i * 32 + lane) : 0.0f;
+      for (int i = 0; i < 8; i++) x[i] = exists<MODE>(i, left) ? __ldcs(p + element<MODE>(i)) : 0.0f;
     }
   } else {
-    const unsigned short* p = static_cast<const unsigned short*>(base) + at;
-    if (VEC) {
-      widen8(__ldcs(reinterpret_cast<const uint4*>(p) + lane), x);
+    const unsigned short* p = static_cast<const unsigned short*>(base);
+    if (MODE == VECTORS) {
+      widen8(__ldcs(reinterpret_cast<const uint4*>(p) + threadIdx.x), x);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; i++) x[i] = i * 32 + lane < left ? __uint_as_float((unsigned)__ldcs(p + i * 32 + lane) << 16) : 0.0f;
+      for (int i = 0; i < 8; i++) x[i] = exists<MODE>(i, left) ? __uint_as_float((unsigned)__ldcs(p + element<MODE>(i)) << 16) : 0.0f;
     }
   }
 }
-// A lane's eight gradients: as vectors of 16 bytes where they can be, so that those of several ranks fit the registers.
-template <int DT, bool VEC>
+// A thread's eight gradients: as vectors of 16 bytes where they can be, so that those of several ranks fit the registers.
+template <int DT, Mode MODE>
 struct Raw {
   float x[8];
-  __device__ __forceinline__ void load(const void* base, unsigned long long at, unsigned left, int lane) { load_floats<DT, VEC>(base, at, left, lane, x); }
+  __device__ __forceinline__ void load(const void* base, unsigned left) { load_floats<DT, MODE>(base, left, x); }
   __device__ __forceinline__ void widen(float* y) const {
 #pragma unroll
     for (int i = 0; i < 8; i++) y[i] = x[i];
   }
 };
 template <>
-struct Raw<1, true> {
+struct Raw<1, VECTORS> {
   uint4 r;
-  __device__ __forceinline__ void load(const void* base, unsigned long long at, unsigned, int lane) {
-    r = __ldcs(reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(base) + at) + lane);
-  }
+  __device__ __forceinline__ void load(const void* base, unsigned) { r = __ldcs(static_cast<const uint4*>(base) + threadIdx.x); }
   __device__ __forceinline__ void widen(float* y) const { widen8(r, y); }
 };
-template <int DT, bool VEC>
-__device__ __forceinline__ void store_floats(void* base, unsigned long long at, unsigned left, int lane, const float* x) {
+template <int DT, Mode MODE>
+__device__ __forceinline__ void store_floats(void* base, unsigned left, const float* x) {
   if (DT == 0) {
-    float* p = static_cast<float*>(base) + at;
-    if (VEC) {
-      store8(p + lane * 8, x);
+    float* p = static_cast<float*>(base);
+    if (MODE == VECTORS) {
+      store8(p + threadIdx.x * 8, x);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++)
-        if (i * 32 + lane < left) __stcs(p + i * 32 + lane, x[i]);
+        if (exists<MODE>(i, left)) __stcs(p + element<MODE>(i), x[i]);
     }
   } else {
-    unsigned short* p = static_cast<unsigned short*>(base) + at;
-    if (VEC) {
-      __stcs(reinterpret_cast<uint4*>(p) + lane, make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])));
+    unsigned short* p = static_cast<unsigned short*>(base);
+    if (MODE == VECTORS) {
+      __stcs(reinterpret_cast<uint4*>(p) + threadIdx.x, make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])));
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++)
-        if (i * 32 + lane < left) __stcs(p + i * 32 + lane, __bfloat16_as_ushort(__float2bfloat16_rn(x[i])));
+        if (exists<MODE>(i, left)) __stcs(p + element<MODE>(i), __bfloat16_as_ushort(__float2bfloat16_rn(x[i])));
     }
   }
 }
 
 // ---------------------------------------------------------------- device: 8-bit states
 
-// The 32-bit finalizer of MurmurHash3 (Appleby, public domain).
-__device__ __forceinline__ unsigned mix(unsigned h) {
+// The 32-bit finalizer of MurmurHash3 (Appleby, public domain), as far as before its last step, h ^ (h >> 16).
+__device__ __forceinline__ unsigned mix_most(unsigned h) {
   h = (h ^ (h >> 16)) * 0x85EBCA6Bu;
-  h = (h ^ (h >> 13)) * 0xC2B2AE35u;
+  return (h ^ (h >> 13)) * 0xC2B2AE35u;
+}
+__device__ __forceinline__ unsigned mix(unsigned h) {
+  h = mix_most(h);
   return h ^ (h >> 16);
 }
 __device__ __forceinline__ unsigned tensor_key(unsigned seed, unsigned tensor) { return mix(seed + tensor * 0x9E3779B9u); }
-__device__ __forceinline__ unsigned element_word(unsigned key, unsigned long long i) { return mix((unsigned)i + (unsigned)(i >> 32) * 0x632BE5ABu + key); }
+// The two halves of a finished word: what m and what the root are rounded with.  (h >> 16 as a permutation of bytes: the shift would be merged with the one
+// that places the bits, and the mask that this needs costs an instruction a number.)
+struct Halves {
+  unsigned m, root;
+};
+__device__ __forceinline__ Halves halves(unsigned h) {
+  h = mix_most(h);
+  const unsigned high = __byte_perm(h, 0, 0x4432);
+  return Halves{(h ^ high) & 0xffffu, high};
+}
+// Of the elements of a tile that starts at element `at` of its tensor: mix(tile_key + offset).  (A tile does not straddle a multiple of 2^32.)
+__device__ __forceinline__ unsigned tile_key(unsigned key, unsigned long long at) { return (unsigned)at + (unsigned)(at >> 32) * 0x632BE5ABu + key; }
 
-template <bool VEC>
-__device__ __forceinline__ void load_codes(const void* base, unsigned long long at, unsigned left, int lane, float scale, float* x) {
-  const unsigned char* p = static_cast<const unsigned char*>(base) + at;
+template <Mode MODE>
+__device__ __forceinline__ void load_codes(const void* base, unsigned left, float scale, float* x) {
+  const unsigned char* p = static_cast<const unsigned char*>(base);
   unsigned short pair[4];
-  if (VEC) {
-    const uint2 r = __ldcs(reinterpret_cast<const uint2*>(p) + lane);
+  if (MODE == VECTORS) {
+    const uint2 r = __ldcs(reinterpret_cast<const uint2*>(p) + threadIdx.x);
     pair[0] = (unsigned short)r.x;
     pair[1] = (unsigned short)(r.x >> 16);
     pair[2] = (unsigned short)r.y;
@@ -238,7 +265,7 @@ __device__ __forceinline__ void load_codes(const void* base, unsigned long long 
   } else {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      const unsigned lo = 2 * i * 32 + lane < left ? __ldcs(p + 2 * i * 32 + lane) : 0, hi = (2 * i + 1) * 32 + lane < left ? __ldcs(p + (2 * i + 1) * 32 + lane) : 0;
+      const unsigned lo = exists<MODE>(2 * i, left) ? __ldcs(p + element<MODE>(2 * i)) : 0, hi = exists<MODE>(2 * i + 1, left) ? __ldcs(p + element<MODE>(2 * i + 1)) : 0;
       pair[i] = (unsigned short)(lo | hi << 8);
     }
   }
@@ -250,17 +277,17 @@ __device__ __forceinline__ void load_codes(const void* base, unsigned long long 
 }
 
 // One number on the grid of e4m3 (3 bits of mantissa from 2^-6 on, steps of 2^-9 below), rounded towards zero or, with the chance of what is
-// cut off, away from it.  rnd: 16 random bits at bits 4 to 19, just below the mantissa's third bit.  Adding 2^-6 to a number below
+// cut off, away from it.  rnd: 16 random bits, which come to lie just below the mantissa's third bit.  Adding 2^-6 to a number below
 // 2^-6 puts it where binary32's own grid of 3 bits has those steps.
-__device__ __forceinline__ float round_normal(float u, unsigned rnd) { return __uint_as_float((__float_as_uint(u) + rnd) & 0xfff00000u); }
+__device__ __forceinline__ float round_normal(float u, unsigned rnd) { return __uint_as_float((__float_as_uint(u) + rnd * 16) & 0xfff00000u); }
 __device__ __forceinline__ float round_any(float u, unsigned rnd) {
   const float shift = fabsf(u) < 0.015625f ? copysignf(0.015625f, u) : 0.0f;
   return copysignf(round_normal(u + shift, rnd) - shift, u);
 }
 // Stores a block (x >= 0 for the root) and its scale.  The whole warp takes part.  A block without a number below 2^-6 of the codes' range, the usual
 // one, does without the steps for those: 4 instructions a number instead of 9.
-template <bool VEC, bool ROOT>
-__device__ __forceinline__ void store_codes(void* base, float* scales, unsigned long long at, unsigned left, int lane, const float* x, const unsigned* word) {
+template <Mode MODE, bool ROOT>
+__device__ __forceinline__ void store_codes(void* base, float* scales, unsigned left, const float* x, const Halves* word) {
   float top = fabsf(x[0]), low = top;
 #pragma unroll
   for (int i = 1; i < 8; i++) {
@@ -270,13 +297,13 @@ __device__ __forceinline__ void store_codes(void* base, float* scales, unsigned 
   top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));   // of non-negative numbers and NaN the words have their order
   const bool some = top > 1e-35f;
   const float inv = some ? __frcp_rn(top) * 448.0f : 0.0f;
-  if (lane == 0) scales[at / kBlock] = some ? top * (1.0f / 448.0f) : top == top ? 0.0f : top;
+  if ((threadIdx.x & 31) == 0) scales[threadIdx.x / 32] = some ? top * (1.0f / 448.0f) : top == top ? 0.0f : top;
   float q[8];
   if (__any_sync(0xffffffffu, low * inv < 0.015625f)) {
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       const float u = x[i] * inv;
-      q[i] = round_any(u, ROOT ? word[i] >> 12 & 0xffff0u : word[i] << 4 & 0xffff0u);
+      q[i] = round_any(u, ROOT ? word[i].root : word[i].m);
       if (ROOT && u > 0.0f) q[i] = fmaxf(q[i], 0.001953125f);
     }
   } else {
@@ -284,19 +311,19 @@ __device__ __forceinline__ void store_codes(void* base, float* scales, unsigned 
     for (int i = 0; i < 8; i += 2) {
       split(mul2(two(x[i], x[i + 1]), two(inv)), q + i);
 #pragma unroll
-      for (int j = i; j < i + 2; j++) q[j] = round_normal(q[j], ROOT ? word[j] >> 12 & 0xffff0u : word[j] << 4 & 0xffff0u);
+      for (int j = i; j < i + 2; j++) q[j] = round_normal(q[j], ROOT ? word[j].root : word[j].m);
     }
   }
   unsigned short pair[4];
 #pragma unroll
   for (int i = 0; i < 4; i++) pair[i] = __nv_cvt_float2_to_fp8x2(make_float2(q[2 * i], q[2 * i + 1]), __NV_SATFINITE, __NV_E4M3);
-  unsigned char* p = static_cast<unsigned char*>(base) + at;
-  if (VEC) {
-    __stcs(reinterpret_cast<uint2*>(p) + lane, make_uint2(pair[0] | (unsigned)pair[1] << 16, pair[2] | (unsigned)pair[3] << 16));
+  unsigned char* p = static_cast<unsigned char*>(base);
+  if (MODE == VECTORS) {
+    __stcs(reinterpret_cast<uint2*>(p) + threadIdx.x, make_uint2(pair[0] | (unsigned)pair[1] << 16, pair[2] | (unsigned)pair[3] << 16));
   } else {
 #pragma unroll
     for (int i = 0; i < 8; i++)
-      if (i * 32 + lane < left) p[i * 32 + lane] = (unsigned char)(pair[i / 2] >> (i % 2 * 8));
+      if (exists<MODE>(i, left)) p[element<MODE>(i)] = (unsigned char)(pair[i / 2] >> (i % 2 * 8));
   }
 }
 
@@ -324,26 +351,44 @@ __device__ __forceinline__ Rates read_rates(const AdamScalars& s) {
   return r;
 }
 
+// The arrays of one tensor (shard) from one tile on.
+struct Place {
+  void *m, *v;
+  float *master, *m_scale, *v_scale;
+  unsigned left, key;   // elements from the tile's start on; tile_key
+};
+__device__ __forceinline__ Place place_of(void* m, void* v, float* master, float* ms, float* vs, unsigned long long n, unsigned long long at, int w, int state,
+                                          unsigned seed, unsigned tensor) {
+  const size_t e = state == HOCCL_STATE_FLOAT32 ? 4 : 1;
+  Place p;
+  p.m = static_cast<char*>(m) + at * e;
+  p.v = static_cast<char*>(v) + at * e;
+  p.master = w == W_MASTER ? master + at : nullptr;
+  p.m_scale = state == HOCCL_STATE_8BIT ? ms + at / kBlock : nullptr;
+  p.v_scale = state == HOCCL_STATE_8BIT ? vs + at / kBlock : nullptr;
+  p.left = (unsigned)min(n - at, (unsigned long long)kTile);
+  p.key = state == HOCCL_STATE_8BIT ? tile_key(tensor_key(seed, tensor), at) : 0;
+  return p;
+}
+
 // What a block's state and weight need besides its gradient.
-template <int W, int STATE, bool VEC>
+template <int W, int STATE, Mode MODE>
 struct Held {
   float p[8], m[8], v[8];
   // weights: W_MASTER from the master, else from param
-  __device__ __forceinline__ void load(const void* param, const float* master, const void* mp, const void* vp, const float* ms, const float* vs,
-                                       unsigned long long weight_at, unsigned long long at, unsigned left, int lane) {
-    if (W == W_MASTER) load_floats<0, VEC>(master, at, left, lane, p);
-    else load_floats<W == W_FP32 ? 0 : 1, VEC>(param, weight_at, left, lane, p);
+  __device__ __forceinline__ void load(const void* param, const Place& a) {
+    if (W == W_MASTER) load_floats<0, MODE>(a.master, a.left, p);
+    else load_floats<W == W_FP32 ? 0 : 1, MODE>(param, a.left, p);
     if (STATE == HOCCL_STATE_FLOAT32) {
-      load_floats<0, VEC>(mp, at, left, lane, m);
-      load_floats<0, VEC>(vp, at, left, lane, v);
+      load_floats<0, MODE>(a.m, a.left, m);
+      load_floats<0, MODE>(a.v, a.left, v);
     } else {
-      load_codes<VEC>(mp, at, left, lane, ms[at / kBlock], m);
-      load_codes<VEC>(vp, at, left, lane, vs[at / kBlock], v);
+      load_codes<MODE>(a.m, a.left, a.m_scale[threadIdx.x / 32], m);
+      load_codes<MODE>(a.v, a.left, a.v_scale[threadIdx.x / 32], v);
     }
   }
   // g: the gradients as they were read.  Afterwards p holds the new weights, which the caller stores; the state is stored here.
-  __device__ __forceinline__ void step(const float* g, const AdamScalars& s, const Rates& r, float keep, unsigned key, float* master, void* mp, void* vp,
-                                       float* ms, float* vs, unsigned long long at, unsigned left, int lane) {
+  __device__ __forceinline__ void step(const float* g, const AdamScalars& s, const Rates& r, float keep, const Place& a) {
     // states: every operation rounded by itself, as the header has it, so that 8-bit codes can be told bit for bit
     float root[8];
     float low = 3.4e38f, high = 0.0f;
@@ -359,7 +404,7 @@ struct Held {
     }
     if (!__any_sync(0xffffffffu, !(low >= kRootLow && high <= kRootHigh))) {
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) split(root_in_range(two(v[i], v[i + 1])), root + i);
+      for (int i = 0; i < 8; i += 2) split(root_in_range(two(v[i], v[i + 1]), two(s.half), two(s.minus_half), two(s.minus_one)), root + i);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++) root[i] = __fsqrt_rn(v[i]);
@@ -372,103 +417,94 @@ struct Held {
       asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(over[1]) : "f"(below[1]));
       split(fma2(mul2(two(m[i], m[i + 1]), two(over[0], over[1])), two(-r.step_size), mul2(two(p[i], p[i + 1]), two(keep))), p + i);
     }
-    if (W == W_MASTER) store_floats<0, VEC>(master, at, left, lane, p);
+    if (W == W_MASTER) store_floats<0, MODE>(a.master, a.left, p);
     if (STATE == HOCCL_STATE_FLOAT32) {
-      store_floats<0, VEC>(mp, at, left, lane, m);
-      store_floats<0, VEC>(vp, at, left, lane, v);
+      store_floats<0, MODE>(a.m, a.left, m);
+      store_floats<0, MODE>(a.v, a.left, v);
     } else {
-      unsigned word[8];
+      Halves word[8];
 #pragma unroll
-      for (int i = 0; i < 8; i++) word[i] = element_word(key, at + element<VEC>(lane, i));
-      store_codes<VEC, false>(mp, ms, at, left, lane, m, word);
-      store_codes<VEC, true>(vp, vs, at, left, lane, root, word);
+      for (int i = 0; i < 8; i++) word[i] = halves(a.key + element<MODE>(i));
+      store_codes<MODE, false>(a.m, a.m_scale, a.left, m, word);
+      store_codes<MODE, true>(a.v, a.v_scale, a.left, root, word);
     }
   }
 };
 
-template <int GT, int W, int STATE, bool VEC>
-__device__ __forceinline__ void tensor_block(const AdamRow& t, const AdamScalars& s, const Rates& r, unsigned block, int lane) {
-  const unsigned long long at = (unsigned long long)block * kBlock;
-  const unsigned left = (unsigned)min(t.n - at, (unsigned long long)kBlock);
-  Held<W, STATE, VEC> h;
+template <int GT, int W, int STATE, Mode MODE>
+__device__ __forceinline__ void tensor_block(const void* grad, void* param, const Place& a, const AdamScalars& s, const Rates& r, float keep) {
+  Held<W, STATE, MODE> h;
   float g[8];
-  load_floats<GT, VEC>(t.grad, at, left, lane, g);
-  h.load(t.param, t.master, t.m, t.v, t.m_scale, t.v_scale, at, at, left, lane);
-  h.step(g, s, r, fmaf(-r.lr, t.decay, 1.0f), STATE == HOCCL_STATE_8BIT ? tensor_key(r.seed, t.flags >> 1) : 0, t.master, t.m, t.v, t.m_scale, t.v_scale, at,
-         left, lane);
-  store_floats<W == W_FP32 ? 0 : 1, VEC>(t.param, at, left, lane, h.p);
+  load_floats<GT, MODE>(grad, a.left, g);
+  h.load(param, a);
+  h.step(g, s, r, keep, a);
+  store_floats<W == W_FP32 ? 0 : 1, MODE>(param, a.left, h.p);
 }
 
 template <int GT, int W, int STATE, class Table>
-__global__ void __launch_bounds__(kOptThreads, 4) adamw_kernel(const __grid_constant__ Table t, const __grid_constant__ AdamScalars s) {
+__global__ void __launch_bounds__(kOptThreads, 32 / kWarps) adamw_kernel(const __grid_constant__ Table t, const __grid_constant__ AdamScalars s) {
   wait_for_stream();
   const Rates r = read_rates(s);
   if (r.skip) return;
-  const int lane = threadIdx.x & 31;
-  const unsigned b0 = (blockIdx.x * kWarps + threadIdx.x / 32) * t.per_warp;
-  if (b0 >= t.blocks) return;
-  const unsigned b1 = min(b0 + t.per_warp, t.blocks);
+  const unsigned tile = blockIdx.x, here = (threadIdx.x & ~31u) * 8;
   int k = 0;
-  for (int step = t.n <= 32 ? 16 : 256; step; step >>= 1)   // the last tensor that starts at or before b0
-    if (k + step < t.n && t.first[k + step] <= b0) k += step;
-  for (unsigned b = b0; b < b1; b++) {
-    while (b >= t.first[k + 1]) k++;
-    const AdamRow& row = t.row[k];
-    const unsigned block = b - t.first[k];
-    if ((row.flags & 1) && (unsigned long long)(block + 1) * kBlock <= row.n) tensor_block<GT, W, STATE, true>(row, s, r, block, lane);
-    else tensor_block<GT, W, STATE, false>(row, s, r, block, lane);
-  }
+  for (int step = t.n <= 32 ? 16 : t.n <= 96 ? 64 : 256; step; step >>= 1)   // the tensor the tile lies in
+    if (k + step < t.n && t.first[k + step] <= tile) k += step;
+  const AdamRow& row = t.row[k];
+  const unsigned long long at = (unsigned long long)(tile - t.first[k]) * kTile;
+  const Place a = place_of(row.m, row.v, row.master, row.m_scale, row.v_scale, row.n, at, W, STATE, r.seed, row.flags >> 1);
+  const void* grad = static_cast<const char*>(row.grad) + at * (GT == 0 ? 4 : 2);
+  void* param = static_cast<char*>(row.param) + at * (W == W_FP32 ? 4 : 2);
+  const float keep = fmaf(-r.lr, row.decay, 1.0f);
+  if (here >= a.left) return;
+  if (here + kBlock > a.left) tensor_block<GT, W, STATE, ENDS>(grad, param, a, s, r, keep);
+  else if (row.flags & 1) tensor_block<GT, W, STATE, VECTORS>(grad, param, a, s, r, keep);
+  else tensor_block<GT, W, STATE, WHOLE>(grad, param, a, s, r, keep);
 }
 
-template <int GT, int W, int STATE, bool VEC>
-__device__ __forceinline__ void sharded_block(const ShardedArgs& a, const AdamScalars& s, const Rates& r, int c, unsigned block, unsigned long long lo,
-                                              unsigned long long n, int lane) {
-  const unsigned long long at = (unsigned long long)block * kBlock;
-  const unsigned left = (unsigned)min(n - at, (unsigned long long)kBlock);
+template <int GT, int W, int STATE, Mode MODE>
+__device__ __forceinline__ void sharded_block(const ShardedArgs& args, const AdamScalars& s, const Rates& r, int c, unsigned long long lo, const Place& a) {
   // the ring's order: c + 1, c + 2, ..., c; the gradients of kFlight ranks in flight at a time, as they lie in memory
-  constexpr int kFlight = !VEC ? 2 : GT == 1 ? 8 : 4;
+  constexpr int kFlight = MODE != VECTORS ? 2 : GT == 1 ? 8 : 4;
   float g[8];
   int from = c;
-  for (int j0 = 0; j0 < a.R; j0 += kFlight) {
-    Raw<GT, VEC> x[kFlight];
+  for (int j0 = 0; j0 < args.R; j0 += kFlight) {
+    Raw<GT, MODE> x[kFlight];
 #pragma unroll
     for (int j = 0; j < kFlight; j++)
-      if (j0 + j < a.R) {
-        from = from + 1 < a.R ? from + 1 : 0;
-        x[j].load(a.grad[from], lo + at, left, lane);
+      if (j0 + j < args.R) {
+        from = from + 1 < args.R ? from + 1 : 0;
+        x[j].load(static_cast<const char*>(args.grad[from]) + lo * (GT == 0 ? 4 : 2), a.left);
       }
 #pragma unroll
     for (int j = 0; j < kFlight; j++)
-      if (j0 + j < a.R) {
+      if (j0 + j < args.R) {
         float y[8];
         x[j].widen(y);
 #pragma unroll
         for (int i = 0; i < 8; i++) g[i] = j0 + j ? __fadd_rn(g[i], y[i]) : y[i];
       }
   }
-  Held<W, STATE, VEC> h;
-  h.load(a.param[c], a.master[c], a.m[c], a.v[c], a.m_scale[c], a.v_scale[c], lo + at, at, left, lane);
-  h.step(g, s, r, fmaf(-r.lr, a.decay, 1.0f), STATE == HOCCL_STATE_8BIT ? tensor_key(r.seed, (unsigned)c) : 0, a.master[c], a.m[c], a.v[c], a.m_scale[c],
-         a.v_scale[c], at, left, lane);
-  for (int to = 0; to < a.R; to++) store_floats<W == W_FP32 ? 0 : 1, VEC>(a.param[to], lo + at, left, lane, h.p);
+  constexpr int kWeight = W == W_FP32 ? 4 : 2;
+  Held<W, STATE, MODE> h;
+  h.load(static_cast<const char*>(args.param[c]) + lo * kWeight, a);
+  h.step(g, s, r, fmaf(-r.lr, args.decay, 1.0f), a);
+  for (int to = 0; to < args.R; to++) store_floats<W == W_FP32 ? 0 : 1, MODE>(static_cast<char*>(args.param[to]) + lo * kWeight, a.left, h.p);
 }
 
 template <int GT, int W, int STATE>
-__global__ void __launch_bounds__(kOptThreads, 2) sharded_adamw_kernel(const __grid_constant__ ShardedArgs a, const __grid_constant__ AdamScalars s) {
+__global__ void __launch_bounds__(kOptThreads, 24 / kWarps) sharded_adamw_kernel(const __grid_constant__ ShardedArgs args, const __grid_constant__ AdamScalars s) {
   wait_for_stream();
   const Rates r = read_rates(s);
   if (r.skip) return;
-  const int lane = threadIdx.x & 31;
-  const unsigned long long total = (unsigned long long)a.per_rank * a.R;
-  const unsigned long long b0 = ((unsigned long long)blockIdx.x * kWarps + threadIdx.x / 32) * a.per_warp;
-  for (unsigned long long b = b0; b < min(b0 + a.per_warp, total); b++) {
-    const int c = (int)(b / a.per_rank);
-    const unsigned block = (unsigned)(b - (unsigned long long)c * a.per_rank);
-    const unsigned long long lo = min(c * a.q, a.count), n = min(a.q, a.count - lo);
-    if ((unsigned long long)block * kBlock >= n) continue;   // the short chunks at the end have fewer blocks
-    if ((a.aligned >> c & 1) && (unsigned long long)(block + 1) * kBlock <= n) sharded_block<GT, W, STATE, true>(a, s, r, c, block, lo, n, lane);
-    else sharded_block<GT, W, STATE, false>(a, s, r, c, block, lo, n, lane);
-  }
+  const unsigned here = (threadIdx.x & ~31u) * 8;
+  const int c = (int)(blockIdx.x / args.per_rank);
+  const unsigned long long at = (unsigned long long)(blockIdx.x - c * args.per_rank) * kTile, lo = min(c * args.q, args.count), n = min(args.q, args.count - lo);
+  if (at + here >= n) return;   // the short chunks at the end have fewer tiles
+  const Place a = place_of(args.m[c], args.v[c], args.master[c], args.m_scale[c], args.v_scale[c], n, at, W, STATE, r.seed, (unsigned)c);
+  if (here + kBlock > a.left) sharded_block<GT, W, STATE, ENDS>(args, s, r, c, lo + at, a);
+  else if (args.aligned >> c & 1) sharded_block<GT, W, STATE, VECTORS>(args, s, r, c, lo + at, a);
+  else sharded_block<GT, W, STATE, WHOLE>(args, s, r, c, lo + at, a);
 }
 
 // ---------------------------------------------------------------- device: the norm
@@ -577,7 +613,7 @@ __global__ void __launch_bounds__(256) root_selftest_kernel(unsigned long long* 
   unsigned long long wrong = 0, seen = 0;
   for (unsigned b = lo + blockIdx.x * 256 + threadIdx.x; b <= hi; b += gridDim.x * 256) {
     float r[2];
-    split(root_in_range(two(__uint_as_float(b), __uint_as_float(hi - (b - lo)))), r);
+    split(root_in_range(two(__uint_as_float(b), __uint_as_float(hi - (b - lo))), two(0.5f), two(-0.5f), two(-1.0f)), r);
     wrong += __float_as_uint(r[0]) != __float_as_uint(__fsqrt_rn(__uint_as_float(b)));
     wrong += __float_as_uint(r[1]) != __float_as_uint(__fsqrt_rn(__uint_as_float(hi - (b - lo))));
     seen++;
@@ -606,11 +642,6 @@ const void* norm_entry(int dtype, bool small) {
   return dtype ? reinterpret_cast<const void*>(&norm_kernel<1, NormTable>) : reinterpret_cast<const void*>(&norm_kernel<0, NormTable>);
 }
 
-// Blocks of one warp: one while the whole GPU has warps to spare for that, then as many as keep the launch at 16 waves.
-unsigned blocks_per_warp(unsigned long long blocks) {
-  const unsigned long long wave = (unsigned long long)kAllSms * 32;
-  return (unsigned)std::min<unsigned long long>(std::max<unsigned long long>(blocks / (16 * wave), 1), 1u << 20);
-}
 bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 bool fill_scalars(const hoccl_adamw_config_t& c, AdamScalars* s) {
@@ -623,17 +654,27 @@ bool fill_scalars(const hoccl_adamw_config_t& c, AdamScalars* s) {
   s->lr = (float)c.lr;
   s->step_size = (float)(c.lr / bias1);
   s->root_scale = (float)(1.0 / std::sqrt(bias2));
-  s->beta1 = (float)c.beta1;
-  s->grad1 = (float)(1.0 - c.beta1);
-  s->beta2 = (float)c.beta2;
-  s->grad2 = (float)(1.0 - c.beta2);
-  s->eps = (float)c.eps;
+  const float eps = (float)c.eps;
+  const auto pair = [](double x) {
+    const float f = (float)x;
+    unsigned w;
+    std::memcpy(&w, &f, 4);
+    return Pair{(unsigned long long)w << 32 | w};
+  };
+  s->beta1 = pair(c.beta1);
+  s->grad1 = pair(1.0 - c.beta1);
+  s->beta2 = pair(c.beta2);
+  s->grad2 = pair(1.0 - c.beta2);
+  s->eps = pair(c.eps);
+  s->one = pair(1.0);
+  s->half = pair(0.5);
+  s->minus_half = pair(-0.5);
+  s->minus_one = pair(-1.0);
   s->grad_scale = (float)c.grad_scale;
-  s->one = 1.0f;
   s->seed = c.seed;
   s->factor = c.factor;
   s->rates = c.rates;
-  return s->eps >= 1.17549435e-38f;   // the kernels divide by numbers from eps on with a reciprocal that takes normal ones
+  return eps >= 1.17549435e-38f;   // the kernels divide by numbers from eps on with a reciprocal that takes normal ones
 }
 
 struct Region {
@@ -682,7 +723,7 @@ void add_optim_kernels(std::vector<const void*>* fns) {
   for (int gt = 0; gt < 2; gt++) {
     for (int w = 0; w < 3; w++)
       for (int state = 0; state < 2; state++)
-        for (const void* f : {adamw_entry<AdamTableSmall>(gt, w, state), adamw_entry<AdamTable>(gt, w, state), sharded_entry(gt, w, state)}) fns->push_back(f);
+        for (const void* f : {adamw_entry<AdamTableSmall>(gt, w, state), adamw_entry<AdamTableMiddle>(gt, w, state), adamw_entry<AdamTable>(gt, w, state), sharded_entry(gt, w, state)}) fns->push_back(f);
     for (bool small : {false, true}) fns->push_back(norm_entry(gt, small));
   }
   fns->push_back(reinterpret_cast<const void*>(&norm_end_kernel));
@@ -694,12 +735,13 @@ void add_optim_kernels(std::vector<const void*>* fns) {
 struct hoccl_adamw_plan {
   int grad_dtype, weights, state;
   std::vector<AdamTableSmall> small;
+  std::vector<AdamTableMiddle> middle;
   std::vector<AdamTable> large;
 };
 
 namespace {
 
-constexpr size_t kMaxTensorElements = 1ull << 39;   // blocks are counted in 32 bits
+constexpr size_t kMaxTensorElements = 1ull << 39;   // 2^28 tiles; with those of 64 ranks' chunks a grid's 2^31 hold them
 
 template <class Table>
 void append_table(const std::vector<AdamRow>& rows, size_t from, size_t n, std::vector<Table>* out) {
@@ -707,14 +749,11 @@ void append_table(const std::vector<AdamRow>& rows, size_t from, size_t n, std::
   Table& t = out->back();
   t.n = (int)n;
   t.pad = 0;
-  t.blocks = 0;
+  t.first[0] = 0;
   for (size_t k = 0; k < n; k++) {
     t.row[k] = rows[from + k];
-    t.first[k] = t.blocks;
-    t.blocks += (unsigned)((t.row[k].n + kBlock - 1) / kBlock);
+    t.first[k + 1] = t.first[k] + (unsigned)((t.row[k].n + kTile - 1) / kTile);
   }
-  t.first[n] = t.blocks;
-  t.per_warp = blocks_per_warp(t.blocks);
 }
 
 hoccl_result_t make_plan(hoccl_adamw_plan_t* out, const hoccl_adamw_tensor_t* tensors, int n, int param_dtype, int grad_dtype, int state) {
@@ -742,17 +781,19 @@ hoccl_result_t make_plan(hoccl_adamw_plan_t* out, const hoccl_adamw_tensor_t* te
   p->grad_dtype = grad_dtype;
   p->state = state;
   p->weights = param_dtype == HOCCL_FLOAT32 ? W_FP32 : with ? W_MASTER : W_BF16;
-  constexpr size_t kLarge = sizeof(AdamTable::row) / sizeof(AdamRow), kSmall = sizeof(AdamTableSmall::row) / sizeof(AdamRow);
+  constexpr size_t kLarge = sizeof(AdamTable::row) / sizeof(AdamRow), kMiddle = sizeof(AdamTableMiddle::row) / sizeof(AdamRow),
+                   kSmall = sizeof(AdamTableSmall::row) / sizeof(AdamRow);
   for (size_t from = 0; from < rows.size();) {
-    unsigned long long blocks = 0;
-    size_t here = 0;   // as many as a table and 32 bits of blocks hold
+    unsigned long long tiles = 0;
+    size_t here = 0;   // as many as a table and a grid hold
     while (here < kLarge && from + here < rows.size()) {
-      const unsigned long long more = (rows[from + here].n + kBlock - 1) / kBlock;
-      if (here && blocks + more > 1ull << 31) break;
-      blocks += more;
+      const unsigned long long more = (rows[from + here].n + kTile - 1) / kTile;
+      if (here && tiles + more >= 1ull << 31) break;
+      tiles += more;
       here++;
     }
     if (here <= kSmall) append_table(rows, from, here, &p->small);
+    else if (here <= kMiddle) append_table(rows, from, here, &p->middle);
     else append_table(rows, from, here, &p->large);
     from += here;
   }
@@ -763,8 +804,7 @@ template <class Table>
 cudaError_t launch_tables(const std::vector<Table>& tables, const hoccl_adamw_plan& p, AdamScalars* s, cudaStream_t stream) {
   for (const Table& t : tables) {
     void* params[2] = {const_cast<Table*>(&t), s};
-    const unsigned long long warps = (t.blocks + t.per_warp - 1) / t.per_warp;
-    const cudaError_t e = launch_in_order_params(adamw_entry<Table>(p.grad_dtype, p.weights, p.state), (int)((warps + kWarps - 1) / kWarps), kOptThreads, params, stream);
+    const cudaError_t e = launch_in_order_params(adamw_entry<Table>(p.grad_dtype, p.weights, p.state), (int)t.first[t.n], kOptThreads, params, stream);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -805,6 +845,7 @@ hoccl_result_t hoccl_adamw_step(hoccl_adamw_plan_t plan, const hoccl_adamw_confi
   DeviceScope scope(c->device);
   CU_TRY(c, scope.err);
   CU_TRY(c, launch_tables(plan->small, *plan, &s, (cudaStream_t)stream));
+  CU_TRY(c, launch_tables(plan->middle, *plan, &s, (cudaStream_t)stream));
   CU_TRY(c, launch_tables(plan->large, *plan, &s, (cudaStream_t)stream));
   c->stats.host_launch_us = now_us() - t0;
   return HOCCL_OK;
@@ -828,8 +869,7 @@ hoccl_result_t hoccl_sharded_adamw(const void* const* grads, void* const* params
   a.decay = weight_decay;
   a.count = count;
   a.q = (count + (size_t)c->R - 1) / (size_t)c->R;
-  a.per_rank = (unsigned)((a.q + kBlock - 1) / kBlock);
-  a.per_warp = blocks_per_warp((unsigned long long)a.per_rank * a.R);
+  a.per_rank = (unsigned)((a.q + kTile - 1) / kTile);
   try {
     std::vector<Region> regions;
     for (int r = 0; r < c->R; r++) {
@@ -856,10 +896,9 @@ hoccl_result_t hoccl_sharded_adamw(const void* const* grads, void* const* params
   }
   DeviceScope scope(c->device);
   CU_TRY(c, scope.err);
-  const unsigned long long warps = ((unsigned long long)a.per_rank * a.R + a.per_warp - 1) / a.per_warp;
   void* launch[2] = {&a, &s};
   const int weights = param_dtype == HOCCL_FLOAT32 ? W_FP32 : master ? W_MASTER : W_BF16;
-  CU_TRY(c, launch_in_order_params(sharded_entry((int)grad_dtype, weights, (int)state), (int)((warps + kWarps - 1) / kWarps), kOptThreads, launch, (cudaStream_t)stream));
+  CU_TRY(c, launch_in_order_params(sharded_entry((int)grad_dtype, weights, (int)state), (int)(a.per_rank * (unsigned)c->R), kOptThreads, launch, (cudaStream_t)stream));
   c->stats.host_launch_us = now_us() - t0;
   return HOCCL_OK;
 }

@@ -189,7 +189,7 @@ def test_first_step_from_zero(comm, state):
     s.check(s.now(), 1e-3, 1, 0.1, 1.0, 1)
 
 
-@pytest.mark.parametrize("n", [31, 33, 420, 421, 900])
+@pytest.mark.parametrize("n", [31, 33, 96, 97, 420, 421, 900])
 @pytest.mark.parametrize("state", ["fp32", "8bit"])
 def test_many_tensors(comm, n, state):
     """More than one table, and both of their sizes."""
