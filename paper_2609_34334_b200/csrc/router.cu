@@ -20,19 +20,24 @@ using namespace hoccl;
 namespace hoccl {
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kMaxExperts = 1024, kMaxTopk = 32;
 constexpr int kRouteThreads = 256, kRouteWarps = kRouteThreads / 32;   // of a CTA whose lanes hold up to 16 logits; half for 32
 template <int V>
 constexpr int kWarpsFor = V <= 16 ? kRouteWarps : kRouteWarps / 2;
 constexpr int kRouteCtas = 4 * kAllSms;          // CTAs of a forward launch besides one for each rank: bounds the scratch
 constexpr int kEndCtas = 8;                      // one cluster
+constexpr int kClusterRanks = 8;                 // ranks up to which a grid may be one cluster that ends by itself
 
 struct RouteArgs {
   int R, experts, topk, groups;
   unsigned long long ld, dld;
   unsigned rows_per_cta;
   int normalize;
-  float* partial;                // forward: 2 * experts + 2 words for each CTA: sums of p, counts, rows, sum of squared logarithms
+  double balance, z, per_choice; // forward: balance_coef * experts, z_coef, 1 / topk
+  float* partial;                // forward: see PartialSums; null if the grid is one cluster, which needs none
+  float *loss, *saved_out;       // forward
   const float* saved;            // backward
   const float* dloss;
   unsigned first[kMaxRanks + 1]; // prefix sums of CTAs
@@ -40,15 +45,7 @@ struct RouteArgs {
   const void* logits[kMaxRanks];
   int* indices[kMaxRanks];
   float* weights[kMaxRanks];     // backward: their gradients
-  void* dlogits[kMaxRanks];
-};
-struct RouteEndArgs {
-  int R, experts, topk, groups;
-  double balance, z;             // balance_coef * experts, z_coef
-  const float* partial;
-  float *loss, *saved;
-  unsigned first[kMaxRanks + 1];
-  int* counts[kMaxRanks];
+  void* dlogits[kMaxRanks];      // forward: the counts
 };
 
 // Over the L lanes of a row; a NaN counts only where there is nothing else.
@@ -114,43 +111,201 @@ __device__ __forceinline__ void load_row(const void* base, unsigned long long at
   }
 }
 
-// Row whose largest logit is `top`: x -> exp(x - top); inv = 1 / their sum; the logarithm of the sum of exp(logit).  A row without a logit above -infinity:
-// 0, NaN where the logit is, inv 1, logarithm 0 (top is set to 0).
+// Row whose largest logit is `top`: x -> exp(x - top); their sum and its reciprocal.  A row without a logit above -infinity:
+// 0, NaN where the logit is, inv 1, and false (top is set to 0).
 template <int V, int L>
-__device__ __forceinline__ void softmax_row(float* x, float* top, float* log_sum, float* inv) {
+__device__ __forceinline__ bool softmax_row(float* x, float* top, float* total, float* inv) {
   const bool open = *top > -INFINITY;
   if (!open) *top = 0.0f;
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < V; i++) sum += x[i] = __expf(x[i] - *top);
   sum = lanes_sum<L>(sum);
-  *inv = open ? 1.0f / sum : 1.0f;
-  *log_sum = open ? *top + logf(sum) : 0.0f;
+  *inv = open ? __fdividef(1.0f, sum) : 1.0f;
+  *total = sum;
+  return open;
+}
+
+// What the CTAs of a forward launch leave for its end: sums of p, counts of the chosen, rows and the sum of squared logarithms.  In memory,
+// CTA after CTA, or in the shared memory of a grid that is one cluster.
+struct PartialSums {
+  const float* at;
+  int experts;
+  __device__ __forceinline__ const float* of(unsigned cta) const { return at + cta * (2 * (size_t)experts + 2); }
+  __device__ __forceinline__ float p(unsigned cta, int e) const { return __ldcg(of(cta) + e); }
+  __device__ __forceinline__ int count(unsigned cta, int e) const { return __float_as_int(__ldcg(of(cta) + experts + e)); }
+  __device__ __forceinline__ float squares(unsigned cta) const { return __ldcg(of(cta) + 2 * experts + 1); }
+};
+struct ClusterSums {
+  float *sums, *sq;   // this CTA's
+  int* counts;
+  int experts;
+  template <class T>
+  __device__ __forceinline__ static T* of(T* own, unsigned cta) {
+    return gridDim.x > 1 ? cg::this_cluster().map_shared_rank(own, cta) : own;
+  }
+  __device__ __forceinline__ float p(unsigned cta, int e) const { return of(sums, cta)[e]; }
+  __device__ __forceinline__ int count(unsigned cta, int e) const { return of(counts, cta)[e]; }
+  __device__ __forceinline__ float squares(unsigned cta) const { return *of(sq, cta); }
+};
+
+// Adds the CTAs' sums in a fixed order.  The CTAs of one cluster take 32 experts at a time each, a lane each; a CTA's warps share the ranks, and a rank's forward
+// CTAs where there are fewer ranks than warps, so that all reads are in flight at once.  The first CTA adds the parts of the loss.
+// shared: end_words(R, warps) words.
+__host__ __device__ constexpr int end_words(int R, int warps) { return 3 * kMaxRanks + 64 * R + 64 * warps; }
+template <class Sums>
+__device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, int ctas, float* shared) {
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
+  int* rows = reinterpret_cast<int*>(shared);           // [kMaxRanks]
+  float *logs = shared + kMaxRanks, *loss = logs + kMaxRanks;
+  float* p_rank = loss + kMaxRanks;                     // [R][32]
+  int* c_rank = reinterpret_cast<int*>(p_rank + 32 * a.R);
+  float* p_part = p_rank + 64 * a.R;                    // [warps][32]
+  int* c_part = reinterpret_cast<int*>(p_part + 32 * warps);
+  int split = 1;
+  while (split * 2 * a.R <= warps) split *= 2;          // warps of one rank
+  for (int g = threadIdx.x; g < a.groups; g += blockDim.x) loss[g] = 0;
+  for (int r = warp; r < a.R; r += warps) {             // every CTA needs the ranks' rows
+    int n = 0;
+    float z = 0;
+    for (unsigned b0 = a.first[r] + lane; b0 < a.first[r + 1]; b0 += 4 * 32) {
+      int ns[4];
+      float zs[4];
+#pragma unroll
+      for (int u = 0; u < 4; u++) {
+        const unsigned b = b0 + u * 32;
+        ns[u] = b < a.first[r + 1] ? in.count(b, a.experts) : 0;
+        zs[u] = b < a.first[r + 1] ? in.squares(b) : 0.0f;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; u++) {
+        n += ns[u];
+        z += zs[u];
+      }
+    }
+    n = __reduce_add_sync(0xffffffffu, n);
+    z = lanes_sum<32>(z);
+    if (lane == 0) {
+      rows[r] = n;
+      logs[r] = z;
+    }
+  }
+  for (int e0 = 32 * (int)blockIdx.x; e0 < a.experts; e0 += 32 * ctas) {
+    const int e = e0 + lane;
+    for (int r0 = 0; r0 < a.R; r0 += warps / split) {
+      const int r = r0 + warp / split;
+      float p = 0;
+      int n = 0;
+      if (r < a.R && e < a.experts) {
+        for (unsigned b0 = a.first[r] + warp % split; b0 < a.first[r + 1]; b0 += 16 * split) {   // 32 reads in flight: the latency of one counts
+          float ps[16];
+          int ns[16];
+#pragma unroll
+          for (int u = 0; u < 16; u++) {
+            const unsigned b = b0 + u * split;
+            ps[u] = b < a.first[r + 1] ? in.p(b, e) : 0.0f;
+            ns[u] = b < a.first[r + 1] ? in.count(b, e) : 0;
+          }
+#pragma unroll
+          for (int u = 0; u < 16; u++) {
+            p += ps[u];
+            n += ns[u];
+          }
+        }
+      }
+      if (split > 1) {
+        p_part[warp * 32 + lane] = p;
+        c_part[warp * 32 + lane] = n;
+        __syncthreads();
+        if (warp % split == 0 && r < a.R)
+          for (int w = 1; w < split; w++) {
+            p += p_part[(warp + w) * 32 + lane];
+            n += c_part[(warp + w) * 32 + lane];
+          }
+      }
+      if (warp % split == 0 && r < a.R) {
+        p_rank[r * 32 + lane] = p;
+        c_rank[r * 32 + lane] = n;
+        if (e < a.experts) static_cast<int*>(a.dlogits[r])[e] = n;
+      }
+    }
+    __syncthreads();
+    for (int g = warp; g < a.groups; g += warps) {
+      const int r0 = a.groups > 1 ? g : 0, r1 = a.groups > 1 ? g + 1 : a.R;
+      float p = 0;
+      long long c = 0, n = 0;
+      for (int r = r0; r < r1; r++) {
+        p += p_rank[r * 32 + lane];
+        c += c_rank[r * 32 + lane];
+        n += rows[r];
+      }
+      const double per_row = n ? 1.0 / (double)n : 0.0, f = (double)c * per_row * a.per_choice;   // rounded to binary32 once
+      if (e < a.experts) a.saved_out[(size_t)g * (a.experts + 1) + e] = (float)(a.balance * f * per_row);
+      const float part = lanes_sum<32>(n ? (float)(f * per_row) * p : p);   // no rows: 0, or NaN
+      if (lane == 0) loss[g] += part;
+    }
+    __syncthreads();
+  }
+  if (ctas > 1) cg::this_cluster().sync();
+  else __syncthreads();
+  if (blockIdx.x == 0) {
+    for (int r = threadIdx.x; r < a.R; r += blockDim.x) static_cast<int*>(a.dlogits[r])[a.experts] = rows[r];
+    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
+      const int r0 = a.groups > 1 ? g : 0, r1 = a.groups > 1 ? g + 1 : a.R;
+      float z = 0, l = 0;
+      long long n = 0;
+      for (int r = r0; r < r1; r++) {
+        z += logs[r];
+        n += rows[r];
+      }
+      if (ctas > 1)
+        for (int c = 0; c < ctas; c++) l += *cg::this_cluster().map_shared_rank(&loss[g], c);
+      else l = loss[g];
+      const double per_row = n ? 1.0 / (double)n : 0.0;
+      a.loss[2 * g] = (float)(a.balance * l);
+      a.loss[2 * g + 1] = (float)(a.z * per_row * z);
+      a.saved_out[(size_t)g * (a.experts + 1) + a.experts] = (float)(2.0 * a.z * per_row);
+    }
+  }
+  if (ctas > 1) cg::this_cluster().sync();               // the others' shared memory lives until it has been read
+}
+
+__global__ void __launch_bounds__(1024) route_end_kernel(const __grid_constant__ RouteArgs a) {
+  __shared__ float shared[end_words(kMaxRanks, 32)];
+  wait_for_stream();
+  route_end(a, PartialSums{a.partial, a.experts}, gridDim.x, shared);
 }
 
 // The topk largest of a row without a pass over it for each: the topk-th largest of the lanes' own largest logits is a bar that at least topk logits reach, and
-// few more do (a dozen for 8 of 256); those are collected and each counts the ones in front of it.  (One search of the whole row for each choice took
-// 1090 instructions a row of 256 and 50 us for 32,000 rows, most of it on the half-rate integer pipe.)
+// few more do (a dozen for 8 of 256); those are collected.  Where a lane can hold each of them and no two are alike, a maximum over the warp finds one after
+// the other; else each counts the ones in front of it.  (One search of the whole row for each choice took 1090 instructions a row of 256 and 50 us for
+// 32,000 rows, most of it on the half-rate integer pipe.)
 template <int DT, int V, int L, bool VEC>
 __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_constant__ RouteArgs a) {
-  constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;   // rows of a warp, of the CTA, at a time
+  constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;     // rows of a warp, of the CTA, at a time
   constexpr int K = L * V < kMaxTopk ? L * V : kMaxTopk;
-  __shared__ __align__(16) uint2 found[kRows][L * V];            // {bits of the logit, expert} of a row's candidates
+  constexpr int kFound = kRows * L * V;
+  __shared__ __align__(16) uint2 found[kFound];                  // {bits of the logit, expert} of a row's candidates, L * V for each row
   __shared__ int count[L * V + 1];
   __shared__ uint2 chosen[kRows][K];
+  __shared__ int candidates[kRows];
   __shared__ float squares[W];
+  static_assert(2 * kFound >= W * L * V + end_words(kClusterRanks, W), "the sums and their end reuse the candidates' room");
   const int warp = threadIdx.x / 32, lane = threadIdx.x % L, group = threadIdx.x % 32 / L, slot = warp * G + group;
+  uint2* mine = found + slot * (L * V);
   for (int e = threadIdx.x; e <= a.experts; e += W * 32) count[e] = 0;
+  if (lane == 0) candidates[slot] = 0;
   int r = 0;
   while (blockIdx.x >= a.first[r + 1]) r++;
   const unsigned row0 = (blockIdx.x - a.first[r]) * a.rows_per_cta, row1 = min(a.tokens[r], row0 + a.rows_per_cta);
   wait_for_stream();
   __syncthreads();
-  float p_sum[V] = {}, z_sum = 0.0f;
+  float p_sum[V] = {}, z_sum = 0.0f, log_top = 0.0f, log_total = 1.0f;   // the last: of one of the rows since their logarithms were taken
+  int turn = 0;
   for (unsigned base = row0 + warp * G; base < row1; base += kRows) {
     const unsigned row = base + group;
     const bool real = row < row1;
-    float x[V], log_sum, inv;
+    float x[V], total, inv;
     if (real) {
       load_row<DT, V, L, VEC>(a.logits[r], row * a.ld, a.experts, lane, x);
     } else {
@@ -163,53 +318,100 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_c
       bar = lanes_max<L>(best);
     }
     bar = fmaxf(bar, -3.402823466e38f);
-    int n = 0;
+    int here = 0;
 #pragma unroll
-    for (int i = 0; i < V; i++) {
-      const bool in = x[i] >= bar;
-      const unsigned all = __ballot_sync(0xffffffffu, in), mine = L == 32 ? all : all >> (group * L) & ((1u << (L & 31)) - 1);
-      if (in) found[slot][n + __popc(mine & ((1u << lane) - 1))] = make_uint2(__float_as_uint(x[i]), expert_of<V, L, VEC>(lane, i));
-      n += __popc(mine);
+    for (int i = 0; i < V; i++) here += x[i] >= bar;
+    if (here) {   // their order does not matter
+      uint2* to = mine + atomicAdd(&candidates[slot], here);
+#pragma unroll
+      for (int i = 0; i < V; i++)
+        if (x[i] >= bar) *to++ = make_uint2(__float_as_uint(x[i]), expert_of<V, L, VEC>(lane, i));
     }
     __syncwarp();
-    softmax_row<V, L>(x, &top, &log_sum, &inv);
+    const int n = candidates[slot], have = min(n, a.topk);
+    const bool open = softmax_row<V, L>(x, &top, &total, &inv);
 #pragma unroll
     for (int i = 0; i < V; i++) p_sum[i] += x[i] * inv;
-    z_sum += log_sum * log_sum;
-    for (int c = lane; c < n; c += L) {
-      const uint2 own = found[slot][c];
+    if (lane == turn) {                  // a logarithm takes as long for one lane as for all: each lane keeps a row's until all have one
+      log_top = top;
+      log_total = open ? total : 1.0f;
+    }
+    if (++turn == L) {
+      const float s = log_top + logf(log_total);
+      z_sum += s * s;
+      log_top = 0.0f;
+      log_total = 1.0f;
+      turn = 0;
+    }
+    const unsigned long long at = (unsigned long long)row * a.topk;
+    bool done = false;
+    if (L == 32 && n <= 32) {            // (the same for the whole warp)
+      const uint2 own = lane < n ? mine[lane] : make_uint2(0xff800000u, 0);
       const float y = __uint_as_float(own.x);
-      int before = 0;
-      for (int j = 0; j < n; j++) {
-        const uint2 o = found[slot][j];
-        before += __uint_as_float(o.x) > y || (__uint_as_float(o.x) == y && o.y < own.y);
-      }
-      if (before < a.topk) {
-        chosen[slot][before] = own;
-        atomicAdd(&count[own.y], 1);
+      float v = y;
+      int rank = -1;
+      for (int k = 0; k < have; k++)
+        if (v == lanes_max<L>(v)) {
+          rank = k;
+          v = -INFINITY;
+        }
+      if (__popc(__ballot_sync(0xffffffffu, rank >= 0)) == have) {   // else equal ones fell together
+        const float ex = __expf(y - top);
+        // 0 * inv: a NaN in the row reaches its weights either way
+        const float scale = a.normalize ? __fdividef(1.0f, lanes_sum<L>(rank >= 0 ? ex : 0.0f)) + 0.0f * inv : inv;
+        if (rank >= 0) {
+          a.indices[r][at + rank] = (int)own.y;
+          a.weights[r][at + rank] = ex * scale;
+          atomicAdd(&count[own.y], 1);
+        }
+        if (lane >= have && lane < a.topk && real) {
+          a.indices[r][at + lane] = -1;
+          a.weights[r][at + lane] = 0.0f;
+        }
+        done = true;
       }
     }
-    if (lane == 0 && n) atomicAdd(&count[a.experts], 1);
-    __syncwarp();
-    const int have = min(n, a.topk);
-    float part = 0.0f;
-    if (a.normalize) {
-      for (int k = lane; k < have; k += L) part += __expf(__uint_as_float(chosen[slot][k].x) - top);
-      part = lanes_sum<L>(part);
-    }
-    if (real) {
-      const float scale = a.normalize ? 1.0f / part + 0.0f * inv : inv;   // a NaN in the row reaches its weights either way
-      for (int k = lane; k < a.topk; k += L) {
-        const unsigned long long at = (unsigned long long)row * a.topk + k;
-        a.indices[r][at] = k < have ? (int)chosen[slot][k].y : -1;
-        a.weights[r][at] = k < have ? __expf(__uint_as_float(chosen[slot][k].x) - top) * scale : 0.0f;
+    if (!done) {
+      for (int c = lane; c < n; c += L) {
+        const uint2 own = mine[c];
+        const float y = __uint_as_float(own.x);
+        int before = 0;
+        for (int j = 0; j < n; j++) {
+          const uint2 o = mine[j];
+          before += __uint_as_float(o.x) > y || (__uint_as_float(o.x) == y && o.y < own.y);
+        }
+        if (before < a.topk) {
+          chosen[slot][before] = own;
+          atomicAdd(&count[own.y], 1);
+        }
       }
+      __syncwarp();
+      float part = 0.0f;
+      if (a.normalize) {
+        for (int k = lane; k < have; k += L) part += __expf(__uint_as_float(chosen[slot][k].x) - top);
+        part = lanes_sum<L>(part);
+      }
+      if (real) {
+        const float scale = a.normalize ? __fdividef(1.0f, part) + 0.0f * inv : inv;
+        for (int k = lane; k < a.topk; k += L) {
+          a.indices[r][at + k] = k < have ? (int)chosen[slot][k].y : -1;
+          a.weights[r][at + k] = k < have ? __expf(__uint_as_float(chosen[slot][k].x) - top) * scale : 0.0f;
+        }
+      }
+    }
+    if (lane == 0) {
+      candidates[slot] = 0;
+      if (n) atomicAdd(&count[a.experts], 1);
     }
     __syncwarp();
   }
+  {
+    const float s = log_top + logf(log_total);
+    z_sum += s * s;
+  }
   // the CTA's sums: lanes of one expert, then warps, in order
   __syncthreads();
-  float* sums = reinterpret_cast<float*>(found);   // [W][experts]
+  float* sums = reinterpret_cast<float*>(found);   // [W][experts], the first one the CTA's in the end
 #pragma unroll
   for (int i = 0; i < V; i++) {
 #pragma unroll
@@ -217,128 +419,34 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_c
     const int e = expert_of<V, L, VEC>(lane, i);
     if (group == 0 && e < a.experts) sums[warp * a.experts + e] = p_sum[i];
   }
-#pragma unroll
-  for (int d = L; d < 32; d <<= 1) z_sum += __shfl_xor_sync(0xffffffffu, z_sum, d);
+  z_sum = lanes_sum<32>(z_sum);
   if (threadIdx.x % 32 == 0) squares[warp] = z_sum;
   __syncthreads();
-  float* out = a.partial + (size_t)blockIdx.x * (2 * a.experts + 2);
+  float* out = a.partial ? a.partial + (size_t)blockIdx.x * (2 * a.experts + 2) : nullptr;
   for (int e = threadIdx.x; e < a.experts; e += W * 32) {
     float s = 0.0f;
     for (int w = 0; w < W; w++) s += sums[w * a.experts + e];
-    out[e] = s;
-    out[a.experts + e] = __int_as_float(count[e]);
+    if (out) {
+      out[e] = s;
+      out[a.experts + e] = __int_as_float(count[e]);
+    } else {
+      sums[e] = s;
+    }
   }
   if (threadIdx.x == 0) {
     float z = 0.0f;
     for (int w = 0; w < W; w++) z += squares[w];
-    out[2 * a.experts] = __int_as_float(count[a.experts]);
-    out[2 * a.experts + 1] = z;
-  }
-}
-
-// Adds the CTAs' sums.  One cluster of one or kEndCtas CTAs; a CTA takes 32 experts at a time, a lane each.  Its 32 warps share the ranks, and the forward CTAs
-// of a rank where there are fewer ranks than warps, so that all loads are in flight at once; the first CTA adds the parts of the loss.
-__global__ void __launch_bounds__(1024) route_end_kernel(const __grid_constant__ RouteEndArgs a) {
-  namespace cg = cooperative_groups;
-  __shared__ float p_part[32][32];
-  __shared__ int c_part[32][32];
-  __shared__ double p_rank[kMaxRanks][32];
-  __shared__ int c_rank[kMaxRanks][32];
-  __shared__ int rows[kMaxRanks];
-  __shared__ double logs[kMaxRanks], loss[kMaxRanks];
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  cg::cluster_group cluster = cg::this_cluster();
-  const int ctas = gridDim.x;
-  int split = 1;
-  while (split * 2 * a.R <= 32) split *= 2;      // warps of one rank
-  if (threadIdx.x < kMaxRanks) loss[threadIdx.x] = 0;
-  wait_for_stream();
-  const size_t words = 2 * (size_t)a.experts + 2;
-  for (int r = warp; r < a.R; r += 32) {         // every CTA needs the ranks' rows
-    int n = 0;
-    double z = 0;
-    for (unsigned b = a.first[r] + lane; b < a.first[r + 1]; b += 32) {
-      const float2 end = make_float2(__ldcg(a.partial + b * words + 2 * a.experts), __ldcg(a.partial + b * words + 2 * a.experts + 1));
-      n += __float_as_int(end.x);
-      z += end.y;
-    }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) {
-      n += __shfl_xor_sync(0xffffffffu, n, d);
-      z += __shfl_xor_sync(0xffffffffu, z, d);
-    }
-    if (lane == 0) {
-      rows[r] = n;
-      logs[r] = z;
+    if (out) {
+      out[2 * a.experts] = __int_as_float(count[a.experts]);
+      out[2 * a.experts + 1] = z;
+    } else {
+      squares[0] = z;
     }
   }
-  for (int e0 = 32 * blockIdx.x; e0 < a.experts; e0 += 32 * ctas) {
-    const int e = e0 + lane;
-    for (int r0 = 0; r0 < a.R; r0 += 32 / split) {
-      const int r = r0 + warp / split;
-      float p = 0;
-      int n = 0;
-      if (r < a.R && e < a.experts) {
-        const float* from = a.partial + e;
-#pragma unroll 4
-        for (unsigned b = a.first[r] + warp % split; b < a.first[r + 1]; b += split) {
-          p += __ldcg(from + b * words);
-          n += __float_as_int(__ldcg(from + b * words + a.experts));
-        }
-      }
-      p_part[warp][lane] = p;
-      c_part[warp][lane] = n;
-      __syncthreads();
-      if (warp % split == 0 && r < a.R) {
-        double sum = 0;
-        n = 0;
-        for (int w = 0; w < split; w++) {
-          sum += p_part[warp + w][lane];
-          n += c_part[warp + w][lane];
-        }
-        p_rank[r][lane] = sum;
-        c_rank[r][lane] = n;
-        if (e < a.experts) a.counts[r][e] = n;
-      }
-      __syncthreads();
-    }
-    for (int g = warp; g < a.groups; g += 32) {
-      const int r0 = a.groups > 1 ? g : 0, r1 = a.groups > 1 ? g + 1 : a.R;
-      double p = 0;
-      long long c = 0, n = 0;
-      for (int r = r0; r < r1; r++) {
-        p += p_rank[r][lane];
-        c += c_rank[r][lane];
-        n += rows[r];
-      }
-      const double f = n ? (double)c / ((double)a.topk * n) : 0;
-      if (e < a.experts) a.saved[(size_t)g * (a.experts + 1) + e] = (float)(n ? a.balance * f / n : 0);
-      double part = n ? f * p / n : p;           // no rows: 0, or NaN
-#pragma unroll
-      for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
-      if (lane == 0) loss[g] += part;
-    }
-    __syncthreads();
-  }
-  if (ctas > 1) cluster.sync();
+  if (out) return;
+  if (gridDim.x > 1) cg::this_cluster().sync();
   else __syncthreads();
-  if (blockIdx.x == 0) {
-    for (int r = threadIdx.x; r < a.R; r += 1024) a.counts[r][a.experts] = rows[r];
-    for (int g = threadIdx.x; g < a.groups; g += 1024) {
-      const int r0 = a.groups > 1 ? g : 0, r1 = a.groups > 1 ? g + 1 : a.R;
-      double z = 0, l = 0;
-      long long n = 0;
-      for (int r = r0; r < r1; r++) {
-        z += logs[r];
-        n += rows[r];
-      }
-      for (int c = 0; c < ctas; c++) l += ctas > 1 ? *cluster.map_shared_rank(&loss[g], c) : loss[g];
-      a.loss[2 * g] = (float)(a.balance * l);
-      a.loss[2 * g + 1] = (float)(n ? a.z * z / n : 0);
-      a.saved[(size_t)g * (a.experts + 1) + a.experts] = (float)(n ? 2 * a.z / n : 0);
-    }
-  }
-  if (ctas > 1) cluster.sync();                  // the others' shared memory lives until it has been read
+  route_end(a, ClusterSums{sums, squares, count, a.experts}, gridDim.x, sums + W * L * V);
 }
 
 template <int DT>
@@ -380,7 +488,7 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_backward_kernel(const
       e = a.indices[r][chosen_at + lane];
       dw = a.weights[r][chosen_at + lane];
     }
-    float x[V], log_sum, inv;
+    float x[V], total, inv;
     if (real) {
       load_row<DT, V, L, VEC>(a.logits[r], logits_at, a.experts, lane, x);
     } else {
@@ -390,12 +498,12 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_backward_kernel(const
     const bool valid = (unsigned)e < (unsigned)a.experts;
     if (valid) y = logit_at<DT>(a.logits[r], logits_at + e);
     float top = lanes_max<L>(largest<V>(x));
-    softmax_row<V, L>(x, &top, &log_sum, &inv);
+    const bool open = softmax_row<V, L>(x, &top, &total, &inv);
     float mean = 0.0f;   // of c under p
 #pragma unroll
     for (int i = 0; i < V; i++) mean += (x[i] *= inv) * c[i];
     mean = lanes_sum<L>(mean);
-    float shift = mean - z * log_sum;
+    float shift = mean - (z != 0.0f && open ? z * (top + logf(total)) : 0.0f);
     if (with) {
       float w = 0.0f, dws = 0.0f;   // sums of p and of p * dw over this lane's choices
       if (alone) {
@@ -572,19 +680,23 @@ hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* t
   const size_t e = dtype_size((int)f->dtype);
   const int shape = shape_of(f->experts), groups = f->per_rank ? c->R : 1;
   RouteArgs a = {};
-  RouteEndArgs end = {};
-  a.R = end.R = c->R;
-  a.experts = end.experts = f->experts;
-  a.topk = end.topk = f->topk;
-  a.groups = end.groups = groups;
+  a.R = c->R;
+  a.experts = f->experts;
+  a.topk = f->topk;
+  a.groups = groups;
   a.ld = ld;
   a.normalize = f->normalize;
+  a.balance = f->balance_coef * f->experts;
+  a.z = f->z_coef;
+  a.per_choice = 1.0 / f->topk;
+  a.loss = loss;
+  a.saved_out = saved;
   bool vec = (f->experts * e) % 16 == 0 && (ld * e) % 16 == 0;
   try {
     std::vector<Span> spans = {{(const char*)loss, 8u * (size_t)groups, true}, {(const char*)saved, (size_t)groups * (f->experts + 1) * 4, true}};
     for (int r = 0; r < c->R; r++) {
       if (!counts[r] || !aligned_to(counts[r], 4)) return HOCCL_ERR_INVALID_ARG;
-      end.counts[r] = counts[r];
+      a.dlogits[r] = counts[r];
       spans.push_back({(const char*)counts[r], (size_t)(f->experts + 1) * 4, true});
       if (!tokens[r]) continue;
       if (!logits[r] || !indices[r] || !weights[r] || !aligned_to(logits[r], e) || !aligned_to(indices[r], 4) || !aligned_to(weights[r], 4)) return HOCCL_ERR_INVALID_ARG;
@@ -603,24 +715,20 @@ hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* t
   }
   const unsigned grid = share_rows(tokens, c->R, shape, kRouteCtas, &a.rows_per_cta, a.first);
   const size_t need = (size_t)grid * (2 * (size_t)f->experts + 2) * sizeof(float);
+  const bool one_cluster = grid && grid <= (unsigned)kEndCtas && c->R <= kClusterRanks;   // ends by itself
   if (need && (!c->scratch || c->scratch_bytes < need)) return HOCCL_ERR_SCRATCH;
-  std::copy(a.first, a.first + kMaxRanks + 1, end.first);
-  a.partial = static_cast<float*>(c->scratch);
-  end.partial = a.partial;
-  end.balance = f->balance_coef * f->experts;
-  end.z = f->z_coef;
-  end.loss = loss;
-  end.saved = saved;
+  a.partial = one_cluster ? nullptr : static_cast<float*>(c->scratch);
   c->stats = hoccl_stats_t{};
   DeviceScope scope(c->device);
   CU_TRY(c, scope.err);
-  if (grid) {
-    CU_TRY(c, launch_in_order(route_entry((int)f->dtype, shape, vec, false), (int)grid, 32 * warps_of(shape), &a, (cudaStream_t)stream));
+  void* params[1] = {&a};
+  if (grid)
+    CU_TRY(c, launch_in_order_params(route_entry((int)f->dtype, shape, vec, false), (int)grid, 32 * warps_of(shape), params, (cudaStream_t)stream, 0, one_cluster ? (int)grid : 1));
+  if (!one_cluster) {
+    // few sums are read by one CTA in less time than a cluster takes to start and meet
+    const int ctas = (size_t)grid * f->experts <= 16384 ? 1 : std::min(kEndCtas, (f->experts + 31) / 32);
+    CU_TRY(c, launch_in_order_params(reinterpret_cast<const void*>(&route_end_kernel), ctas, 1024, params, (cudaStream_t)stream, 0, ctas));
   }
-  // few sums are read by one CTA in less time than a cluster takes to start and meet
-  const int ctas = (size_t)grid * f->experts <= 16384 ? 1 : std::min(kEndCtas, (f->experts + 31) / 32);
-  void* params[1] = {&end};
-  CU_TRY(c, launch_in_order_params(reinterpret_cast<const void*>(&route_end_kernel), ctas, 1024, params, (cudaStream_t)stream, 0, ctas));
   c->stats.host_launch_us = now_us() - t0;
   return HOCCL_OK;
 }
