@@ -129,6 +129,7 @@ __device__ __forceinline__ bool softmax_row(float* x, float* top, float* total, 
 // What the CTAs of a forward launch leave for its end: sums of p, counts of the chosen, rows and the sum of squared logarithms.  In memory,
 // CTA after CTA, or in the shared memory of a grid that is one cluster.
 struct PartialSums {
+  static constexpr int kFlight = 16;   // CTAs whose sums a thread has on their way at a time: the latency of one counts
   const float* at;
   int experts;
   __device__ __forceinline__ const float* of(unsigned cta) const { return at + cta * (2 * (size_t)experts + 2); }
@@ -136,39 +137,42 @@ struct PartialSums {
   __device__ __forceinline__ int count(unsigned cta, int e) const { return __float_as_int(__ldcg(of(cta) + experts + e)); }
   __device__ __forceinline__ float squares(unsigned cta) const { return __ldcg(of(cta) + 2 * experts + 1); }
 };
+template <class T>
+__device__ __forceinline__ T* in_cluster(T* own, unsigned cta) {
+  return gridDim.x > 1 ? cg::this_cluster().map_shared_rank(own, cta) : own;
+}
 struct ClusterSums {
+  static constexpr int kFlight = 1;
   float *sums, *sq;   // this CTA's
   int* counts;
   int experts;
-  template <class T>
-  __device__ __forceinline__ static T* of(T* own, unsigned cta) {
-    return gridDim.x > 1 ? cg::this_cluster().map_shared_rank(own, cta) : own;
-  }
-  __device__ __forceinline__ float p(unsigned cta, int e) const { return of(sums, cta)[e]; }
-  __device__ __forceinline__ int count(unsigned cta, int e) const { return of(counts, cta)[e]; }
-  __device__ __forceinline__ float squares(unsigned cta) const { return *of(sq, cta); }
+  __device__ __forceinline__ float p(unsigned cta, int e) const { return in_cluster(sums, cta)[e]; }
+  __device__ __forceinline__ int count(unsigned cta, int e) const { return in_cluster(counts, cta)[e]; }
+  __device__ __forceinline__ float squares(unsigned cta) const { return *in_cluster(sq, cta); }
 };
 
-// Adds the CTAs' sums in a fixed order.  The CTAs of one cluster take 32 experts at a time each, a lane each; a CTA's warps share the ranks, and a rank's forward
-// CTAs where there are fewer ranks than warps, so that all reads are in flight at once.  The first CTA adds the parts of the loss.
+// Adds the CTAs' sums in a fixed order.  The CTAs of the grid, one cluster, take 32 experts at a time each, a lane each; a CTA's warps share the ranks, and a rank's
+// forward CTAs where there are fewer ranks than warps.  Each CTA puts its parts of the losses into the first one's shared memory, which adds them.
 // shared: end_words(R, warps) words.
-__host__ __device__ constexpr int end_words(int R, int warps) { return 3 * kMaxRanks + 64 * R + 64 * warps; }
+__host__ __device__ constexpr int end_words(int R, int warps) { return (3 + kEndCtas) * kMaxRanks + kMaxRanks + 64 * R + 64 * warps; }
 template <class Sums>
-__device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, int ctas, float* shared) {
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32;
-  int* rows = reinterpret_cast<int*>(shared);           // [kMaxRanks]
-  float *logs = shared + kMaxRanks, *loss = logs + kMaxRanks;
-  float* p_rank = loss + kMaxRanks;                     // [R][32]
+__device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, float* shared) {
+  constexpr int F = Sums::kFlight;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32, ctas = gridDim.x;
+  double* per_row = reinterpret_cast<double*>(shared);                  // [kMaxRanks]: 1 / rows of a group
+  float* parts = shared + 2 * kMaxRanks;                                // [kEndCtas][kMaxRanks], filled in the first CTA
+  int* rows = reinterpret_cast<int*>(parts + kEndCtas * kMaxRanks);     // [kMaxRanks]
+  float* logs = parts + (kEndCtas + 1) * kMaxRanks;                     // [kMaxRanks]
+  float* p_rank = logs + kMaxRanks;                                     // [R][32]
   int* c_rank = reinterpret_cast<int*>(p_rank + 32 * a.R);
-  float* p_part = p_rank + 64 * a.R;                    // [warps][32]
+  float* p_part = p_rank + 64 * a.R;                                    // [warps][32]
   int* c_part = reinterpret_cast<int*>(p_part + 32 * warps);
   int split = 1;
-  while (split * 2 * a.R <= warps) split *= 2;          // warps of one rank
-  for (int g = threadIdx.x; g < a.groups; g += blockDim.x) loss[g] = 0;
-  for (int r = warp; r < a.R; r += warps) {             // every CTA needs the ranks' rows
+  while (split * 2 * a.R <= warps) split *= 2;                          // warps of one rank
+  for (int r = warp; r < a.R; r += warps) {                             // every CTA needs the ranks' rows
     int n = 0;
     float z = 0;
-    for (unsigned b0 = a.first[r] + lane; b0 < a.first[r + 1]; b0 += 4 * 32) {
+    for (unsigned b0 = a.first[r] + lane; b0 < a.first[r + 1]; b0 += 32 * 4) {
       int ns[4];
       float zs[4];
 #pragma unroll
@@ -190,6 +194,10 @@ __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, in
       logs[r] = z;
     }
   }
+  constexpr int kGroups = 2;                                            // of a warp: 64 ranks on 32 warps, kClusterRanks on 4
+  float loss[kGroups];                                                  // of group warp + i * warps, in this CTA's experts
+#pragma unroll
+  for (int i = 0; i < kGroups; i++) loss[i] = 0.0f;
   for (int e0 = 32 * (int)blockIdx.x; e0 < a.experts; e0 += 32 * ctas) {
     const int e = e0 + lane;
     for (int r0 = 0; r0 < a.R; r0 += warps / split) {
@@ -197,17 +205,17 @@ __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, in
       float p = 0;
       int n = 0;
       if (r < a.R && e < a.experts) {
-        for (unsigned b0 = a.first[r] + warp % split; b0 < a.first[r + 1]; b0 += 16 * split) {   // 32 reads in flight: the latency of one counts
-          float ps[16];
-          int ns[16];
+        for (unsigned b0 = a.first[r] + warp % split; b0 < a.first[r + 1]; b0 += F * split) {
+          float ps[F];
+          int ns[F];
 #pragma unroll
-          for (int u = 0; u < 16; u++) {
+          for (int u = 0; u < F; u++) {
             const unsigned b = b0 + u * split;
             ps[u] = b < a.first[r + 1] ? in.p(b, e) : 0.0f;
             ns[u] = b < a.first[r + 1] ? in.count(b, e) : 0;
           }
 #pragma unroll
-          for (int u = 0; u < 16; u++) {
+          for (int u = 0; u < F; u++) {
             p += ps[u];
             n += ns[u];
           }
@@ -230,50 +238,53 @@ __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, in
       }
     }
     __syncthreads();
-    for (int g = warp; g < a.groups; g += warps) {
+#pragma unroll
+    for (int i = 0; i < kGroups; i++) {
+      const int g = warp + i * warps;
+      if (g >= a.groups) break;
       const int r0 = a.groups > 1 ? g : 0, r1 = a.groups > 1 ? g + 1 : a.R;
       float p = 0;
       long long c = 0, n = 0;
+#pragma unroll 8
       for (int r = r0; r < r1; r++) {
         p += p_rank[r * 32 + lane];
         c += c_rank[r * 32 + lane];
         n += rows[r];
       }
-      const double per_row = n ? 1.0 / (double)n : 0.0, f = (double)c * per_row * a.per_choice;   // rounded to binary32 once
-      if (e < a.experts) a.saved_out[(size_t)g * (a.experts + 1) + e] = (float)(a.balance * f * per_row);
-      const float part = lanes_sum<32>(n ? (float)(f * per_row) * p : p);   // no rows: 0, or NaN
-      if (lane == 0) loss[g] += part;
+      const double each = n ? 1.0 / (double)n : 0.0, f = (double)c * each * a.per_choice;   // rounded to binary32 once
+      if (e < a.experts) a.saved_out[(size_t)g * (a.experts + 1) + e] = (float)(a.balance * f * each);
+      loss[i] += n ? (float)(f * each) * p : p;                         // no rows: 0, or NaN
+      if (lane == 0) per_row[g] = each;
     }
     __syncthreads();
   }
+#pragma unroll
+  for (int i = 0; i < kGroups; i++) {
+    const int g = warp + i * warps;
+    if (g >= a.groups) break;
+    const float part = lanes_sum<32>(loss[i]);
+    if (lane == 0) in_cluster(parts, 0)[blockIdx.x * kMaxRanks + g] = part;
+  }
   if (ctas > 1) cg::this_cluster().sync();
   else __syncthreads();
-  if (blockIdx.x == 0) {
-    for (int r = threadIdx.x; r < a.R; r += blockDim.x) static_cast<int*>(a.dlogits[r])[a.experts] = rows[r];
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
-      const int r0 = a.groups > 1 ? g : 0, r1 = a.groups > 1 ? g + 1 : a.R;
-      float z = 0, l = 0;
-      long long n = 0;
-      for (int r = r0; r < r1; r++) {
-        z += logs[r];
-        n += rows[r];
-      }
-      if (ctas > 1)
-        for (int c = 0; c < ctas; c++) l += *cg::this_cluster().map_shared_rank(&loss[g], c);
-      else l = loss[g];
-      const double per_row = n ? 1.0 / (double)n : 0.0;
-      a.loss[2 * g] = (float)(a.balance * l);
-      a.loss[2 * g + 1] = (float)(a.z * per_row * z);
-      a.saved_out[(size_t)g * (a.experts + 1) + a.experts] = (float)(2.0 * a.z * per_row);
-    }
+  if (blockIdx.x != 0) return;
+  for (int r = threadIdx.x; r < a.R; r += blockDim.x) static_cast<int*>(a.dlogits[r])[a.experts] = rows[r];
+  for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
+    const int r0 = a.groups > 1 ? g : 0, r1 = a.groups > 1 ? g + 1 : a.R;
+    float l = 0.0f, z = 0.0f;
+    for (int c = 0; c < ctas; c++) l += parts[c * kMaxRanks + g];
+#pragma unroll 8
+    for (int r = r0; r < r1; r++) z += logs[r];
+    a.loss[2 * g] = (float)(a.balance * l);
+    a.loss[2 * g + 1] = (float)(a.z * per_row[g] * z);
+    a.saved_out[(size_t)g * (a.experts + 1) + a.experts] = (float)(2.0 * a.z * per_row[g]);
   }
-  if (ctas > 1) cg::this_cluster().sync();               // the others' shared memory lives until it has been read
 }
 
 __global__ void __launch_bounds__(1024) route_end_kernel(const __grid_constant__ RouteArgs a) {
-  __shared__ float shared[end_words(kMaxRanks, 32)];
+  __shared__ __align__(16) float shared[end_words(kMaxRanks, 32)];
   wait_for_stream();
-  route_end(a, PartialSums{a.partial, a.experts}, gridDim.x, shared);
+  route_end(a, PartialSums{a.partial, a.experts}, shared);
 }
 
 // The topk largest of a row without a pass over it for each: the topk-th largest of the lanes' own largest logits is a bar that at least topk logits reach, and
@@ -285,12 +296,13 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_c
   constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;     // rows of a warp, of the CTA, at a time
   constexpr int K = L * V < kMaxTopk ? L * V : kMaxTopk;
   constexpr int kFound = kRows * L * V;
-  __shared__ __align__(16) uint2 found[kFound];                  // {bits of the logit, expert} of a row's candidates, L * V for each row
+  constexpr int kEnd = W * L * V + end_words(kClusterRanks, W);  // words of the sums and of their end, which reuse the candidates' room
+  __shared__ __align__(16) uint2 found[kFound > kEnd / 2 ? kFound : (kEnd + 1) / 2];   // {bits of the logit, expert} of a row's candidates, L * V for each row
   __shared__ int count[L * V + 1];
   __shared__ uint2 chosen[kRows][K];
   __shared__ int candidates[kRows];
   __shared__ float squares[W];
-  static_assert(2 * kFound >= W * L * V + end_words(kClusterRanks, W), "the sums and their end reuse the candidates' room");
+  static_assert(W * L * V % 2 == 0, "8-byte words in the end's room");
   const int warp = threadIdx.x / 32, lane = threadIdx.x % L, group = threadIdx.x % 32 / L, slot = warp * G + group;
   uint2* mine = found + slot * (L * V);
   for (int e = threadIdx.x; e <= a.experts; e += W * 32) count[e] = 0;
@@ -345,30 +357,38 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_c
     }
     const unsigned long long at = (unsigned long long)row * a.topk;
     bool done = false;
-    if (L == 32 && n <= 32) {            // (the same for the whole warp)
+    if (__all_sync(0xffffffffu, n <= L)) {
       const uint2 own = lane < n ? mine[lane] : make_uint2(0xff800000u, 0);
       const float y = __uint_as_float(own.x);
       float v = y;
       int rank = -1;
-      for (int k = 0; k < have; k++)
-        if (v == lanes_max<L>(v)) {
+      for (int k = 0; k < a.topk; k++) {
+        const float most = lanes_max<L>(v);
+        if (v == most && most > -INFINITY && k < have) {
           rank = k;
           v = -INFINITY;
         }
-      if (__popc(__ballot_sync(0xffffffffu, rank >= 0)) == have) {   // else equal ones fell together
+      }
+      // equal ones fell together unless as many have a rank as there are ranks, and one has the last
+      constexpr unsigned kLanes = L == 32 ? 0xffffffffu : (1u << (L & 31)) - 1;
+      const unsigned ranked = __ballot_sync(0xffffffffu, rank >= 0) >> (L == 32 ? 0 : group * L) & kLanes;
+      const unsigned last = __ballot_sync(0xffffffffu, rank == have - 1 && have) >> (L == 32 ? 0 : group * L) & kLanes;
+      done = __all_sync(0xffffffffu, __popc(ranked) == have && (last || !have));
+      if (done) {
         const float ex = __expf(y - top);
         // 0 * inv: a NaN in the row reaches its weights either way
-        const float scale = a.normalize ? __fdividef(1.0f, lanes_sum<L>(rank >= 0 ? ex : 0.0f)) + 0.0f * inv : inv;
+        const float part = a.normalize ? lanes_sum<L>(rank >= 0 ? ex : 0.0f) : 1.0f;
+        const float scale = a.normalize ? __fdividef(1.0f, part) + 0.0f * inv : inv;
         if (rank >= 0) {
           a.indices[r][at + rank] = (int)own.y;
           a.weights[r][at + rank] = ex * scale;
           atomicAdd(&count[own.y], 1);
         }
-        if (lane >= have && lane < a.topk && real) {
-          a.indices[r][at + lane] = -1;
-          a.weights[r][at + lane] = 0.0f;
-        }
-        done = true;
+        if (real)
+          for (int k = lane < have ? lane + L : lane; k < a.topk; k += L) {   // (topk <= L but for few experts)
+            a.indices[r][at + k] = -1;
+            a.weights[r][at + k] = 0.0f;
+          }
       }
     }
     if (!done) {
@@ -446,7 +466,7 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_c
   if (out) return;
   if (gridDim.x > 1) cg::this_cluster().sync();
   else __syncthreads();
-  route_end(a, ClusterSums{sums, squares, count, a.experts}, gridDim.x, sums + W * L * V);
+  route_end(a, ClusterSums{sums, squares, count, a.experts}, sums + W * L * V);
 }
 
 template <int DT>
@@ -584,21 +604,22 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_backward_kernel(const
 
 // ---------------------------------------------------------------- host
 
-// Shapes: 8 logits a lane and as many lanes as the experts need, then 16 and 32 logits a lane.
+// Shapes: as many lanes as there are experts up to 32, from 8 on; then 2, 4, ... 32 logits a lane.
 constexpr int kShapes = 8;
 int shape_of(int experts) {
   int s = 0;
   while ((8 << s) < experts) s++;
   return s;
 }
-int lanes_of(int shape) { return 1 << std::min(shape, 5); }
+int lanes_of(int shape) { return 8 << std::min(shape, 2); }
 int warps_of(int shape) { return shape == 7 ? kRouteWarps / 2 : kRouteWarps; }
 size_t rows_at_once(int shape) { return (size_t)warps_of(shape) * (32 / lanes_of(shape)); }
 
 template <int DT, bool VEC>
 const void* route_entry_of(int shape, bool backward) {
-#define ROW(V, L) {reinterpret_cast<const void*>(&route_kernel<DT, V, L, VEC>), reinterpret_cast<const void*>(&route_backward_kernel<DT, V, L, VEC>)}
-  static const void* const fns[kShapes][2] = {ROW(8, 1), ROW(8, 2), ROW(8, 4), ROW(8, 8), ROW(8, 16), ROW(8, 32), ROW(16, 32), ROW(32, 32)};
+  // a lane's logits are at least a vector of 16 bytes
+#define ROW(V, L) {reinterpret_cast<const void*>(&route_kernel<DT, V, L, (VEC && V >= Traits<DT>::VE)>), reinterpret_cast<const void*>(&route_backward_kernel<DT, V, L, (VEC && V >= Traits<DT>::VE)>)}
+  static const void* const fns[kShapes][2] = {ROW(1, 8), ROW(1, 16), ROW(1, 32), ROW(2, 32), ROW(4, 32), ROW(8, 32), ROW(16, 32), ROW(32, 32)};
 #undef ROW
   return fns[shape][backward];
 }
@@ -648,6 +669,21 @@ unsigned share_rows(const size_t* tokens, int R, int shape, unsigned most, unsig
   first[0] = 0;
   for (int r = 0; r < R; r++) first[r + 1] = first[r] + (unsigned)((tokens[r] + per - 1) / per);
   return first[R];
+}
+
+// The same in one cluster, if its warps have at most kClusterTurns rows then: a second launch costs as much as several rows of a warp (8 ranks of 32 rows of
+// 64 experts: 10.4 us in one cluster with 4 turns, 12.0 us for 33 rows in two launches).
+constexpr int kClusterTurns = 4;
+bool share_in_cluster(const size_t* tokens, int R, int shape, unsigned* rows_per_cta, unsigned* first) {
+  if (R > kClusterRanks) return false;
+  unsigned long long most = 0;
+  for (int r = 0; r < R; r++) most = std::max<unsigned long long>(most, tokens[r]);
+  const unsigned long long at_once = rows_at_once(shape), ctas = kEndCtas / R, per = std::max(((most + ctas - 1) / ctas + at_once - 1) / at_once, 1ull) * at_once;
+  if (per > kClusterTurns * at_once) return false;
+  *rows_per_cta = (unsigned)per;
+  first[0] = 0;
+  for (int r = 0; r < R; r++) first[r + 1] = first[r] + (unsigned)((tokens[r] + per - 1) / per);
+  return true;
 }
 
 }  // namespace
@@ -713,9 +749,10 @@ hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* t
   } catch (const std::bad_alloc&) {
     return HOCCL_ERR_INTERNAL;
   }
-  const unsigned grid = share_rows(tokens, c->R, shape, kRouteCtas, &a.rows_per_cta, a.first);
+  unsigned grid = share_rows(tokens, c->R, shape, kRouteCtas, &a.rows_per_cta, a.first);
   const size_t need = (size_t)grid * (2 * (size_t)f->experts + 2) * sizeof(float);
-  const bool one_cluster = grid && grid <= (unsigned)kEndCtas && c->R <= kClusterRanks;   // ends by itself
+  const bool one_cluster = grid && share_in_cluster(tokens, c->R, shape, &a.rows_per_cta, a.first);   // ends by itself
+  if (one_cluster) grid = a.first[c->R];
   if (need && (!c->scratch || c->scratch_bytes < need)) return HOCCL_ERR_SCRATCH;
   a.partial = one_cluster ? nullptr : static_cast<float*>(c->scratch);
   c->stats = hoccl_stats_t{};
@@ -725,8 +762,7 @@ hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* t
   if (grid)
     CU_TRY(c, launch_in_order_params(route_entry((int)f->dtype, shape, vec, false), (int)grid, 32 * warps_of(shape), params, (cudaStream_t)stream, 0, one_cluster ? (int)grid : 1));
   if (!one_cluster) {
-    // few sums are read by one CTA in less time than a cluster takes to start and meet
-    const int ctas = (size_t)grid * f->experts <= 16384 ? 1 : std::min(kEndCtas, (f->experts + 31) / 32);
+    const int ctas = std::min(kEndCtas, (f->experts + 31) / 32);   // (one CTA for 256 experts takes 32 us where 8 take 13)
     CU_TRY(c, launch_in_order_params(reinterpret_cast<const void*>(&route_end_kernel), ctas, 1024, params, (cudaStream_t)stream, 0, ctas));
   }
   c->stats.host_launch_us = now_us() - t0;
