@@ -26,7 +26,9 @@ constexpr int kMaxExperts = 1024, kMaxTopk = 32;
 constexpr int kRouteThreads = 256, kRouteWarps = kRouteThreads / 32;   // of a CTA whose lanes hold up to 16 logits; half for 32
 template <int V>
 constexpr int kWarpsFor = V <= 16 ? kRouteWarps : kRouteWarps / 2;
-constexpr int kRouteCtas = 4 * kAllSms;          // CTAs of a forward launch besides one for each rank: bounds the scratch
+template <int V>
+constexpr int kCtasFor = V <= 8 ? 4 : 1;         // of an SM: more, with fewer registers, lose the loads that a thread has on their way
+constexpr int kRouteCtas = 4 * kAllSms;          // CTAs of a launch besides one for each rank, one wave; bounds the scratch
 constexpr int kEndCtas = 8;                      // one cluster
 constexpr int kClusterRanks = 8;                 // ranks up to which a grid may be one cluster that ends by itself
 
@@ -66,6 +68,12 @@ __device__ __forceinline__ float lanes_sum(float x) {
 #pragma unroll
   for (int d = L / 2; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
   return x;
+}
+// e^x, off by 2 + |1.17 x| units in the last place; 0 where that is below the least normal number.
+__device__ __forceinline__ float exp_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f));
+  return r;
 }
 template <int V>
 __device__ __forceinline__ float largest(const float* x) {
@@ -119,7 +127,7 @@ __device__ __forceinline__ bool softmax_row(float* x, float* top, float* total, 
   if (!open) *top = 0.0f;
   float sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < V; i++) sum += x[i] = __expf(x[i] - *top);
+  for (int i = 0; i < V; i++) sum += x[i] = exp_fast(x[i] - *top);
   sum = lanes_sum<L>(sum);
   *inv = open ? __fdividef(1.0f, sum) : 1.0f;
   *total = sum;
@@ -292,7 +300,7 @@ __global__ void __launch_bounds__(1024) route_end_kernel(const __grid_constant__
 // the other; else each counts the ones in front of it.  (One search of the whole row for each choice took 1090 instructions a row of 256 and 50 us for
 // 32,000 rows, most of it on the half-rate integer pipe.)
 template <int DT, int V, int L, bool VEC>
-__global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_constant__ RouteArgs a) {
+__global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_kernel(const __grid_constant__ RouteArgs a) {
   constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;     // rows of a warp, of the CTA, at a time
   constexpr int K = L * V < kMaxTopk ? L * V : kMaxTopk;
   constexpr int kFound = kRows * L * V;
@@ -334,10 +342,10 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_c
 #pragma unroll
     for (int i = 0; i < V; i++) here += x[i] >= bar;
     if (here) {   // their order does not matter
-      uint2* to = mine + atomicAdd(&candidates[slot], here);
+      int to = slot * (L * V) + atomicAdd(&candidates[slot], here);
 #pragma unroll
       for (int i = 0; i < V; i++)
-        if (x[i] >= bar) *to++ = make_uint2(__float_as_uint(x[i]), expert_of<V, L, VEC>(lane, i));
+        if (x[i] >= bar) found[to++] = make_uint2(__float_as_uint(x[i]), expert_of<V, L, VEC>(lane, i));
     }
     __syncwarp();
     const int n = candidates[slot], have = min(n, a.topk);
@@ -358,24 +366,22 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_c
     const unsigned long long at = (unsigned long long)row * a.topk;
     bool done = false;
     if (__all_sync(0xffffffffu, n <= L)) {
-      const uint2 own = lane < n ? mine[lane] : make_uint2(0xff800000u, 0);
+      const uint2 own = lane < n ? mine[lane] : make_uint2(0x7fc00000u, 0);
       const float y = __uint_as_float(own.x);
-      float v = y;
+      float v = y;   // NaN: none, or taken
       int rank = -1;
-      for (int k = 0; k < a.topk; k++) {
-        const float most = lanes_max<L>(v);
-        if (v == most && most > -INFINITY && k < have) {
+      for (int k = 0; k < a.topk; k++)
+        if (v == lanes_max<L>(v)) {
           rank = k;
-          v = -INFINITY;
+          v = __uint_as_float(0x7fc00000u);
         }
-      }
       // equal ones fell together unless as many have a rank as there are ranks, and one has the last
       constexpr unsigned kLanes = L == 32 ? 0xffffffffu : (1u << (L & 31)) - 1;
       const unsigned ranked = __ballot_sync(0xffffffffu, rank >= 0) >> (L == 32 ? 0 : group * L) & kLanes;
       const unsigned last = __ballot_sync(0xffffffffu, rank == have - 1 && have) >> (L == 32 ? 0 : group * L) & kLanes;
       done = __all_sync(0xffffffffu, __popc(ranked) == have && (last || !have));
       if (done) {
-        const float ex = __expf(y - top);
+        const float ex = exp_fast(y - top);
         // 0 * inv: a NaN in the row reaches its weights either way
         const float part = a.normalize ? lanes_sum<L>(rank >= 0 ? ex : 0.0f) : 1.0f;
         const float scale = a.normalize ? __fdividef(1.0f, part) + 0.0f * inv : inv;
@@ -408,14 +414,14 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_kernel(const __grid_c
       __syncwarp();
       float part = 0.0f;
       if (a.normalize) {
-        for (int k = lane; k < have; k += L) part += __expf(__uint_as_float(chosen[slot][k].x) - top);
+        for (int k = lane; k < have; k += L) part += exp_fast(__uint_as_float(chosen[slot][k].x) - top);
         part = lanes_sum<L>(part);
       }
       if (real) {
         const float scale = a.normalize ? __fdividef(1.0f, part) + 0.0f * inv : inv;
         for (int k = lane; k < a.topk; k += L) {
           a.indices[r][at + k] = k < have ? (int)chosen[slot][k].y : -1;
-          a.weights[r][at + k] = k < have ? __expf(__uint_as_float(chosen[slot][k].x) - top) * scale : 0.0f;
+          a.weights[r][at + k] = k < have ? exp_fast(__uint_as_float(chosen[slot][k].x) - top) * scale : 0.0f;
         }
       }
     }
@@ -477,9 +483,10 @@ __device__ __forceinline__ float logit_at(const void* base, unsigned long long a
 // dlogits_j = p_j (c_j - shift) + what the weights' gradient adds to the chosen.  The latter comes through shared memory, where expert e of a row lies at
 // the place that its lane reads without a bank conflict; what was added is set back to zero behind the row.
 template <int DT, int V, int L, bool VEC>
-__global__ void __launch_bounds__(kWarpsFor<V> * 32) route_backward_kernel(const __grid_constant__ RouteArgs a) {
+__global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_backward_kernel(const __grid_constant__ RouteArgs a) {
   constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;
   __shared__ float extra[kRows][L * V];
+  __shared__ unsigned char seen[kRows][L * V];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % L, group = threadIdx.x % 32 / L, slot = warp * G + group;
   const auto place = [](int e) { return VEC ? e % V * L + e / V : e; };
   int r = 0;
@@ -497,26 +504,35 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_backward_kernel(const
     const int e = expert_of<V, L, VEC>(lane, i);
     c[i] = e < a.experts ? a.saved[(size_t)g * (a.experts + 1) + e] * scale : 0.0f;
   }
+  // a row's logits, this lane's choice of it (expert and gradient of its weight): the next row's are on their way while one is worked on
+  float next[V], next_dw = 0.0f;
+  int next_e = -1;
+  const auto fetch = [&](unsigned row) {
+    next_e = -1;
+    if (row < row1) {
+      if (with && alone && lane < a.topk) {
+        next_e = a.indices[r][(unsigned long long)row * a.topk + lane];
+        next_dw = a.weights[r][(unsigned long long)row * a.topk + lane];
+      }
+      load_row<DT, V, L, VEC>(a.logits[r], row * a.ld, a.experts, lane, next);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; i++) next[i] = -INFINITY;
+    }
+  };
+  fetch(row0 + slot);
   for (unsigned base = row0 + warp * G; base < row1; base += kRows) {
     const unsigned row = base + group;
     const bool real = row < row1;
     const unsigned long long logits_at = row * a.ld, chosen_at = (unsigned long long)row * a.topk;
-    // this lane's choice: expert, gradient of its weight, logit
-    int e = -1;
-    float dw = 0.0f, y = 0.0f;
-    if (with && alone && real && lane < a.topk) {
-      e = a.indices[r][chosen_at + lane];
-      dw = a.weights[r][chosen_at + lane];
-    }
-    float x[V], total, inv;
-    if (real) {
-      load_row<DT, V, L, VEC>(a.logits[r], logits_at, a.experts, lane, x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; i++) x[i] = -INFINITY;
-    }
+    const int e = next_e;
+    const float dw = next_dw;
     const bool valid = (unsigned)e < (unsigned)a.experts;
+    float x[V], total, inv, y = 0.0f;
     if (valid) y = logit_at<DT>(a.logits[r], logits_at + e);
+#pragma unroll
+    for (int i = 0; i < V; i++) x[i] = next[i];
+    fetch(row + kRows);
     float top = lanes_max<L>(largest<V>(x));
     const bool open = softmax_row<V, L>(x, &top, &total, &inv);
     float mean = 0.0f;   // of c under p
@@ -527,13 +543,13 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_backward_kernel(const
     if (with) {
       float w = 0.0f, dws = 0.0f;   // sums of p and of p * dw over this lane's choices
       if (alone) {
-        w = valid ? __expf(y - top) * inv : 0.0f;
+        w = valid ? exp_fast(y - top) * inv : 0.0f;
         dws = valid ? w * dw : 0.0f;
       } else {
         for (int k = lane; k < a.topk && real; k += L) {
           const unsigned i = (unsigned)a.indices[r][chosen_at + k];
           if (i >= (unsigned)a.experts) continue;
-          const float p = __expf(logit_at<DT>(a.logits[r], logits_at + i) - top) * inv;
+          const float p = exp_fast(logit_at<DT>(a.logits[r], logits_at + i) - top) * inv;
           w += p;
           dws += p * a.weights[r][chosen_at + k];
         }
@@ -542,15 +558,20 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32) route_backward_kernel(const
       const float per = a.normalize ? (w_sum > 0.0f ? 1.0f / w_sum : w_sum) : 1.0f;   // 0 or NaN stays
       const float inner = dw_sum * per, less = a.normalize ? inner : 0.0f;
       // an index that comes twice in a row adds twice, one after the other in the order of k
-      const unsigned same = alone ? __match_any_sync(0xffffffffu, valid ? group * kMaxExperts + e : -1 - (int)(threadIdx.x % 32)) : 0;
-      if (alone && !__any_sync(0xffffffffu, (same & (same - 1)) != 0)) {
+      bool twice = false;
+      if (alone) {   // of two lanes that leave their number in one place, one does not find it there
+        if (valid) seen[slot][e] = (unsigned char)lane;
+        __syncwarp();
+        twice = valid && seen[slot][e] != lane;
+      }
+      if (alone && !__any_sync(0xffffffffu, twice)) {
         if (valid) extra[slot][place(e)] = w * per * (dw - less);
       } else {
         for (int k = 0; k < a.topk; k++) {
           if (real && lane == k % L) {
             const unsigned i = (unsigned)a.indices[r][chosen_at + k];
             if (i < (unsigned)a.experts)
-              extra[slot][place((int)i)] += __expf(logit_at<DT>(a.logits[r], logits_at + i) - top) * inv * per * (a.weights[r][chosen_at + k] - less);
+              extra[slot][place((int)i)] += exp_fast(logit_at<DT>(a.logits[r], logits_at + i) - top) * inv * per * (a.weights[r][chosen_at + k] - less);
           }
           __syncwarp();
         }
@@ -671,9 +692,9 @@ unsigned share_rows(const size_t* tokens, int R, int shape, unsigned most, unsig
   return first[R];
 }
 
-// The same in one cluster, if its warps have at most kClusterTurns rows then: a second launch costs as much as several rows of a warp (8 ranks of 32 rows of
-// 64 experts: 10.4 us in one cluster with 4 turns, 12.0 us for 33 rows in two launches).
-constexpr int kClusterTurns = 4;
+// The same in one cluster, if its warps have at most kClusterTurns rows then: a second launch costs as much as a few rows of a warp (8 ranks, 64 experts: 7.4 us
+// for 16 rows in one cluster, 9.2 us for 33 in two launches and as much for 24 in one cluster with 3 turns).
+constexpr int kClusterTurns = 2;
 bool share_in_cluster(const size_t* tokens, int R, int shape, unsigned* rows_per_cta, unsigned* first) {
   if (R > kClusterRanks) return false;
   unsigned long long most = 0;
@@ -815,8 +836,7 @@ hoccl_result_t hoccl_route_backward(const void* const* logits, size_t ld, const 
     return HOCCL_ERR_INTERNAL;
   }
   c->stats = hoccl_stats_t{};
-  // an expert more or less costs the backward kernel no scratch: as many CTAs as two waves hold
-  const unsigned grid = share_rows(tokens, c->R, shape, 8 * kAllSms, &a.rows_per_cta, a.first);
+  const unsigned grid = share_rows(tokens, c->R, shape, kRouteCtas, &a.rows_per_cta, a.first);
   if (!grid) return HOCCL_OK;
   DeviceScope scope(c->device);
   CU_TRY(c, scope.err);
