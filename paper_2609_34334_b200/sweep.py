@@ -6,6 +6,7 @@ pipeline / gradient-stream workloads (third and fourth), through the C ABI.
     python -m paper_2609_34334_b200.sweep gradients [--buckets 32] [--budgets 1,2,4,8,16,32,64]
     python -m paper_2609_34334_b200.sweep launch-cost
     python -m paper_2609_34334_b200.sweep alltoallv [--mib 4,64,256] [--model 4,2]
+    python -m paper_2609_34334_b200.sweep step [--buckets 16]      # the optimizer's part of that stream, and an expert layer's exchange with its router
     python -m paper_2609_34334_b200.sweep cases [--only NAME,NAME] [--draw N --seed S]   # the calls of perf/cases.py, listed and drawn (from the repository's root)
     python -m paper_2609_34334_b200.sweep call --op allreduce --ranks 8 --count 20971520 --dtype bf16 \\
         --variants "ce_overlap=2;ce_overlap=4;path=SM,sum_ctas=8,copy_ctas=40" [--gemm]   # one call under several settings, in turn
@@ -365,6 +366,105 @@ def gradients(args):
         comm.destroy()
 
 
+def _per_call(fn, stream, reps):
+    for _ in range(3):
+        fn(0)
+    stream.synchronize()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    e0.record(stream)
+    for k in range(reps):
+        fn(k)
+    e1.record(stream)
+    stream.synchronize()
+    return e0.elapsed_time(e1) / reps
+
+
+def step(args):
+    """What a training step adds to its collectives.  Optimizer: a bucket of the gradient stream (bf16, R = 8) through the sharded AdamW kernel, and through
+    reduce-scatter, gradient norm, AdamW on the shards and all-gather (the form that clips), with states in 32 and in 8 bits.  Experts: 4096 tokens a rank
+    routed to 64 experts, 8 a rank, the rows exchanged by hoccl_alltoallv with the router's counts, and the router's gradient."""
+    torch.cuda.set_device(0)
+    g = W.C4_GRADIENTS
+    R, n = g.R, g.buckets()[0]
+    q = n // R
+    assert q * R == n
+    stream = torch.cuda.Stream()
+    new = lambda k, dt: torch.zeros(k, dtype=dt, device="cuda")  # noqa: E731
+    pool = 3
+    grads = [[torch.empty(n, dtype=torch.bfloat16, device="cuda").normal_(0, g.sigma) for _ in range(R)] for _ in range(pool)]
+    params = [new(n, torch.bfloat16) for _ in range(R)]
+    shards = [[new(q, torch.bfloat16) for _ in range(R)] for _ in range(pool)]
+    own = [params[r][r * q:(r + 1) * q] for r in range(R)]
+    master = [new(q, torch.float32) for _ in range(R)]
+    comm = hb.Comm(R, 0)
+    nbytes = max(hb.scratch_bytes_direct(R, n, g.dtype), hb.grad_norm_scratch_bytes())
+    scratch = new(nbytes, torch.uint8)
+    comm.set_scratch(scratch, nbytes)
+    norm = new(2, torch.float32)
+    torch.cuda.synchronize()
+    for state in ("fp32", "8bit"):
+        dt = torch.float32 if state == "fp32" else torch.float8_e4m3fn
+        m, v = ([new(q, dt) for _ in range(R)] for _ in range(2))
+        ms, vs = ([new(-(-q // hb.STATE_BLOCK), torch.float32) for _ in range(R)] for _ in range(2))
+        tables = [hb.AdamTensors(own, shards[k], m, v, "bf16", "bf16", state=state, master=master, exp_avg_scale=ms, exp_avg_sq_scale=vs) for k in range(pool)]
+        lists = [hb.Tensors(shards[k], "bf16") for k in range(pool)]
+        torch.cuda.synchronize()
+
+        def fused(k):
+            comm.sharded_adamw(grads[k % pool], params, m, v, n, "bf16", "bf16", 1e-4, k + 1, state=state, master=master, exp_avg_scale=ms, exp_avg_sq_scale=vs,
+                               grad_scale=1.0 / R, seed=k, stream=stream)
+
+        def clipped(k):
+            j = k % pool
+            comm.reduce_scatter(grads[j], shards[j], q, "bf16", stream)
+            comm.grad_norm(lists[j], norm, max_norm=1.0, stream=stream)
+            comm.adamw(tables[j], 1e-4, k + 1, grad_scale=1.0 / R, factor=norm[1:], seed=k, stream=stream)
+            comm.allgather(own, params, q, "bf16", stream)
+
+        state_bytes = 16 if state == "fp32" else 4 + 16 / hb.STATE_BLOCK
+        floor = n * (2 * R + state_bytes + 8 + 2 * R)
+        for name, fn in (("sharded_adamw", fused), ("reduce_scatter+grad_norm+adamw+allgather", clipped)):
+            ms_ = _per_call(fn, stream, args.buckets)
+            print(json.dumps({"workload": g.name, "step": name, "state": state, "bucket_MiB": n * 2 >> 20, "ms_per_bucket": ms_,
+                              "floor_bytes_of_the_fused_form": floor, "GBps_of_that": floor / ms_ / 1e6}), flush=True)
+    comm.destroy()
+    T, width, E, K = 4096, g.hidden, 64, 1
+    comm = hb.Comm(R, 0)
+    nbytes = hb.route_scratch_bytes(R, T, E)
+    scratch = new(nbytes, torch.uint8)
+    comm.set_scratch(scratch, nbytes)
+    logits = [torch.randn(T, E, device="cuda") + torch.randn(E, device="cuda") for _ in range(R)]
+    x = [torch.randn(T, width, device="cuda").bfloat16() for _ in range(R)]
+    indices = [torch.zeros(T, K, dtype=torch.int32, device="cuda") for _ in range(R)]
+    weights, dweights = ([torch.ones(T, K, device="cuda") for _ in range(R)] for _ in range(2))
+    counts, loss, saved = torch.zeros(R, E + 1, dtype=torch.int32, device="cuda"), new(2, torch.float32), new(E + 1, torch.float32)
+    dlogits = [torch.zeros_like(t) for t in logits]
+    torch.cuda.synchronize()
+    tokens = [T] * R
+
+    def route(k):
+        comm.route(logits, tokens, E, K, "fp32", indices, weights, list(counts), loss, saved, z_coef=1e-3, stream=stream)
+
+    def back(k):
+        comm.route_backward(logits, tokens, E, K, "fp32", indices, saved, dweights, None, dlogits, stream=stream)
+
+    t_route, t_back = _per_call(route, stream, 50), _per_call(back, stream, 50)
+    # rank v holds experts v * E / R ...: a rank's rows go out in the order of their experts
+    send = [t[torch.argsort(indices[r][:, 0], stable=True)].contiguous() for r, t in enumerate(x)]
+    c = counts[:, :E].view(R, R, E // R).sum(2).cpu().tolist()
+    sendcounts = [c[u][v] * width for u in range(R) for v in range(R)]
+    sdispls = [sum(c[u][:v]) * width for u in range(R) for v in range(R)]
+    rdispls = [sum(c[a][v] for a in range(u)) * width for v in range(R) for u in range(R)]
+    recv = [new(max(1, sum(c[u][v] for u in range(R)) * width), torch.bfloat16) for v in range(R)]
+    torch.cuda.synchronize()
+    t_exchange = _per_call(lambda k: comm.alltoallv(send, sendcounts, sdispls, recv, rdispls, "bf16", stream), stream, 20)
+    delivered = all(torch.equal(recv[v][rdispls[v * R + u]:rdispls[v * R + u] + c[u][v] * width],
+                                send[u].view(-1)[sdispls[u * R + v]:sdispls[u * R + v] + c[u][v] * width]) for u in range(R) for v in range(R))
+    print(json.dumps({"step": "expert layer", "tokens_per_rank": T, "experts": E, "width": width, "route_us": t_route * 1e3, "alltoallv_us": t_exchange * 1e3,
+                      "route_backward_us": t_back * 1e3, "delivered_bit_exact": delivered, "balance_loss": float(loss[0]), "z_loss": float(loss[1])}), flush=True)
+    comm.destroy()
+
+
 def launch_cost(args):
     """Host time of one all-reduce call against the number of operations it issues (the paper's CPU launch overhead
     axis, Sec. 5): R = 8, 64 MiB bf16 per rank, chunks cut into 1..64 pieces, stream executor against graph replay, with
@@ -639,6 +739,8 @@ def main():
     g.add_argument("--buckets", type=int, default=32)
     g.add_argument("--budgets", default="", help="comma list of copy-kernel CTA budgets, e.g. 1,2,4,8,16,32,64")
     g.add_argument("--ring", action="store_true", help="repeat every configuration on the ring schedule (rs_direct = 0, ag_direct = 0)")
+    s2 = sub.add_parser("step")
+    s2.add_argument("--buckets", type=int, default=16)
     sub.add_parser("launch-cost")
     a2 = sub.add_parser("alltoallv")
     a2.add_argument("--mib", default="4,64,256", help="comma list of MiB sent per rank")
@@ -658,7 +760,7 @@ def main():
     if not torch.cuda.is_available():
         sys.stderr.write("sweep: no CUDA device\n")
         return 2
-    {"sizes": sweep_sizes, "pipeline": pipeline, "gradients": gradients, "launch-cost": launch_cost, "alltoallv": alltoallv, "cases": cases, "call": call}[args.cmd](args)
+    {"sizes": sweep_sizes, "pipeline": pipeline, "gradients": gradients, "step": step, "launch-cost": launch_cost, "alltoallv": alltoallv, "cases": cases, "call": call}[args.cmd](args)
     return 0
 
 
