@@ -674,6 +674,8 @@ bool fill_scalars(const hoccl_adamw_config_t& c, AdamScalars* s) {
   s->seed = c.seed;
   s->factor = c.factor;
   s->rates = c.rates;
+  for (float x : {s->lr, s->step_size, s->root_scale, s->grad_scale})
+    if (!std::isfinite(x)) return false;
   return eps >= 1.17549435e-38f;   // the kernels divide by numbers from eps on with a reciprocal that takes normal ones
 }
 

@@ -302,12 +302,11 @@ __global__ void __launch_bounds__(1024) route_end_kernel(const __grid_constant__
 template <int DT, int V, int L, bool VEC>
 __global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_kernel(const __grid_constant__ RouteArgs a) {
   constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;     // rows of a warp, of the CTA, at a time
-  constexpr int K = L * V < kMaxTopk ? L * V : kMaxTopk;
   constexpr int kFound = kRows * L * V;
   constexpr int kEnd = W * L * V + end_words(kClusterRanks, W);  // words of the sums and of their end, which reuse the candidates' room
   __shared__ __align__(16) uint2 found[kFound > kEnd / 2 ? kFound : (kEnd + 1) / 2];   // {bits of the logit, expert} of a row's candidates, L * V for each row
   __shared__ int count[L * V + 1];
-  __shared__ uint2 chosen[kRows][K];
+  __shared__ uint2 chosen[kRows][L];                              // (topk <= L: see kShapes)
   __shared__ int candidates[kRows];
   __shared__ float squares[W];
   static_assert(W * L * V % 2 == 0, "8-byte words in the end's room");
@@ -390,11 +389,10 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_kernel(c
           a.weights[r][at + rank] = ex * scale;
           atomicAdd(&count[own.y], 1);
         }
-        if (real)
-          for (int k = lane < have ? lane + L : lane; k < a.topk; k += L) {   // (topk <= L but for few experts)
-            a.indices[r][at + k] = -1;
-            a.weights[r][at + k] = 0.0f;
-          }
+        if (real && lane >= have && lane < a.topk) {
+          a.indices[r][at + lane] = -1;
+          a.weights[r][at + lane] = 0.0f;
+        }
       }
     }
     if (!done) {
@@ -412,17 +410,12 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_kernel(c
         }
       }
       __syncwarp();
-      float part = 0.0f;
-      if (a.normalize) {
-        for (int k = lane; k < have; k += L) part += exp_fast(__uint_as_float(chosen[slot][k].x) - top);
-        part = lanes_sum<L>(part);
-      }
-      if (real) {
-        const float scale = a.normalize ? __fdividef(1.0f, part) + 0.0f * inv : inv;
-        for (int k = lane; k < a.topk; k += L) {
-          a.indices[r][at + k] = k < have ? (int)chosen[slot][k].y : -1;
-          a.weights[r][at + k] = k < have ? exp_fast(__uint_as_float(chosen[slot][k].x) - top) * scale : 0.0f;
-        }
+      const uint2 own = lane < have ? chosen[slot][lane] : make_uint2(0, 0xffffffffu);
+      const float ex = lane < have ? exp_fast(__uint_as_float(own.x) - top) : 0.0f;
+      const float part = a.normalize ? lanes_sum<L>(ex) : 1.0f;
+      if (real && lane < a.topk) {
+        a.indices[r][at + lane] = (int)own.y;
+        a.weights[r][at + lane] = lane < have ? ex * (a.normalize ? __fdividef(1.0f, part) + 0.0f * inv : inv) : 0.0f;
       }
     }
     if (lane == 0) {
@@ -492,7 +485,7 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_backward
   int r = 0;
   while (blockIdx.x >= a.first[r + 1]) r++;
   const unsigned row0 = (blockIdx.x - a.first[r]) * a.rows_per_cta, row1 = min(a.tokens[r], row0 + a.rows_per_cta);
-  const bool with = a.weights[r] != nullptr, alone = a.topk <= L;   // a lane holds one of the chosen at most
+  const bool with = a.weights[r] != nullptr;
 #pragma unroll
   for (int i = 0; i < V; i++) extra[slot][i * L + lane] = 0.0f;
   wait_for_stream();
@@ -510,7 +503,7 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_backward
   const auto fetch = [&](unsigned row) {
     next_e = -1;
     if (row < row1) {
-      if (with && alone && lane < a.topk) {
+      if (with && lane < a.topk) {
         next_e = a.indices[r][(unsigned long long)row * a.topk + lane];
         next_dw = a.weights[r][(unsigned long long)row * a.topk + lane];
       }
@@ -524,7 +517,7 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_backward
   for (unsigned base = row0 + warp * G; base < row1; base += kRows) {
     const unsigned row = base + group;
     const bool real = row < row1;
-    const unsigned long long logits_at = row * a.ld, chosen_at = (unsigned long long)row * a.topk;
+    const unsigned long long logits_at = row * a.ld;
     const int e = next_e;
     const float dw = next_dw;
     const bool valid = (unsigned)e < (unsigned)a.experts;
@@ -541,38 +534,19 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_backward
     mean = lanes_sum<L>(mean);
     float shift = mean - (z != 0.0f && open ? z * (top + logf(total)) : 0.0f);
     if (with) {
-      float w = 0.0f, dws = 0.0f;   // sums of p and of p * dw over this lane's choices
-      if (alone) {
-        w = valid ? exp_fast(y - top) * inv : 0.0f;
-        dws = valid ? w * dw : 0.0f;
-      } else {
-        for (int k = lane; k < a.topk && real; k += L) {
-          const unsigned i = (unsigned)a.indices[r][chosen_at + k];
-          if (i >= (unsigned)a.experts) continue;
-          const float p = exp_fast(logit_at<DT>(a.logits[r], logits_at + i) - top) * inv;
-          w += p;
-          dws += p * a.weights[r][chosen_at + k];
-        }
-      }
+      const float w = valid ? exp_fast(y - top) * inv : 0.0f, dws = valid ? w * dw : 0.0f;
       const float w_sum = lanes_sum<L>(w), dw_sum = lanes_sum<L>(dws);
       const float per = a.normalize ? (w_sum > 0.0f ? 1.0f / w_sum : w_sum) : 1.0f;   // 0 or NaN stays
       const float inner = dw_sum * per, less = a.normalize ? inner : 0.0f;
       // an index that comes twice in a row adds twice, one after the other in the order of k
-      bool twice = false;
-      if (alone) {   // of two lanes that leave their number in one place, one does not find it there
-        if (valid) seen[slot][e] = (unsigned char)lane;
-        __syncwarp();
-        twice = valid && seen[slot][e] != lane;
-      }
-      if (alone && !__any_sync(0xffffffffu, twice)) {
-        if (valid) extra[slot][place(e)] = w * per * (dw - less);
+      const float add = w * per * (dw - less);
+      if (valid) seen[slot][e] = (unsigned char)lane;   // of two lanes that leave their number in one place, one does not find it there
+      __syncwarp();
+      if (!__any_sync(0xffffffffu, valid && seen[slot][e] != lane)) {
+        if (valid) extra[slot][place(e)] = add;
       } else {
         for (int k = 0; k < a.topk; k++) {
-          if (real && lane == k % L) {
-            const unsigned i = (unsigned)a.indices[r][chosen_at + k];
-            if (i < (unsigned)a.experts)
-              extra[slot][place((int)i)] += exp_fast(logit_at<DT>(a.logits[r], logits_at + i) - top) * inv * per * (a.weights[r][chosen_at + k] - less);
-          }
+          if (valid && lane == k) extra[slot][place(e)] += add;
           __syncwarp();
         }
       }
@@ -585,12 +559,7 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_backward
 #pragma unroll
       for (int i = 0; i < V; i++) x[i] += extra[slot][i * L + lane];
       __syncwarp();
-      if (alone) {
-        if (valid) extra[slot][place(e)] = 0.0f;
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; i++) extra[slot][i * L + lane] = 0.0f;
-      }
+      if (valid) extra[slot][place(e)] = 0.0f;
       __syncwarp();
     }
     if (real) {
@@ -625,7 +594,8 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_backward
 
 // ---------------------------------------------------------------- host
 
-// Shapes: as many lanes as there are experts up to 32, from 8 on; then 2, 4, ... 32 logits a lane.
+// Shapes: as many lanes as there are experts up to 32, from 8 on; then 2, 4, ... 32 logits a lane.  topk is at most the experts and at most 32, so a lane
+// holds one of a row's chosen.
 constexpr int kShapes = 8;
 int shape_of(int experts) {
   int s = 0;

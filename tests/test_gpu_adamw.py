@@ -455,6 +455,35 @@ def test_sharded_formula(R, n, param, master, grad, state):
     comm.destroy()
 
 
+def test_sharded_with_more_elements_than_32_bits_count():
+    R, n = 2, (1 << 32) + 600
+    q, comm = n // 2, hb.Comm(2, 0)
+    bf = lambda k: [torch.zeros(k, dtype=torch.bfloat16, device="cuda") for _ in range(R)]  # noqa: E731
+    g, p = bf(n), bf(n)
+    m, v = ([torch.zeros(q, dtype=torch.float8_e4m3fn, device="cuda") for _ in range(R)] for _ in range(2))
+    ms, vs = ([torch.zeros(-(-q // BLOCK), device="cuda") for _ in range(R)] for _ in range(2))
+    start = q // BLOCK * BLOCK                      # of rank 1's last block
+    k = q - start
+    x = torch.randn(2, k, generator=torch.Generator().manual_seed(1)).bfloat16()
+    for r in range(R):
+        g[r][n - k:] = x[r].cuda()
+    comm.sharded_adamw(g, p, m, v, n, "bf16", "bf16", 1e-3, 1, state="8bit", exp_avg_scale=ms, exp_avg_sq_scale=vs, beta1=B1, beta2=B2, eps=EPS, seed=4)
+    zero = torch.zeros(k, dtype=torch.float64)
+    s = x.double().sum(0)                           # of two bf16 numbers: one rounding, of at most u of their sizes, in binary32
+    extra = 2.0 ** -24 * x.double().abs().sum(0)
+    wp, wm, wv, ep, em, ev = adamw(zero, s, zero, zero, 1e-3, 1, B1, B2, EPS, 0.0, 1.0)
+    # the first step's quotient is +-1 but for eps: the sum's error moves m and the root alike
+    for r in range(R):
+        assert ((p[r][n - k:].cpu().double() - wp).abs() <= ep + HALF["bf16"] * wp.abs() * 1.01 + 1e-3 * 2 * extra / (s.abs() + EPS)).all()
+        assert not p[r][:n - k].any()
+    w = words(4, 1, k, start)
+    check_codes(m[1][start:].cpu(), ms[1][-1:].cpu(), wm, em + (1 - B1) * extra, w, False)
+    root = wv.sqrt()
+    check_codes(v[1][start:].cpu(), vs[1][-1:].cpu(), root, root * 6 * 2.0 ** -24 + math.sqrt(1 - B2) * extra, w, True)
+    assert not ms[0].any() and not ms[1][:-1].any()
+    comm.destroy()
+
+
 def test_sharded_factor_and_capture():
     R, n = 4, 10_000
     comm = hb.Comm(R, 0)

@@ -91,7 +91,7 @@ def test_plan_checks_tensors():
 
 
 BAD_NUMBERS = [dict(lr=math.nan), dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=math.nan), dict(eps=0.0), dict(eps=1e-60), dict(step=0),
-               dict(step=-3), dict(grad_scale=math.inf), dict(factor=2), dict(rates=8)]
+               dict(step=-3), dict(grad_scale=math.inf), dict(lr=1e39), dict(grad_scale=-1e39), dict(factor=2), dict(rates=8)]
 
 
 @pytest.mark.parametrize("bad", BAD_NUMBERS)
