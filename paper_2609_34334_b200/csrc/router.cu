@@ -23,12 +23,10 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kMaxExperts = 1024, kMaxTopk = 32;
-constexpr int kRouteThreads = 256, kRouteWarps = kRouteThreads / 32;   // of a CTA whose lanes hold up to 16 logits; half for 32
+// Warps of a CTA: many, so that few CTAs leave sums behind (32,000 rows of 256 experts: 28 us with 8, 2x with 16), as far as the candidates' room allows.
 template <int V>
-constexpr int kWarpsFor = V <= 16 ? kRouteWarps : kRouteWarps / 2;
-template <int V>
-constexpr int kCtasFor = V <= 8 ? 4 : 1;         // of an SM: more, with fewer registers, lose the loads that a thread has on their way
-constexpr int kRouteCtas = 4 * kAllSms;          // CTAs of a launch besides one for each rank, one wave; bounds the scratch
+constexpr int kWarpsFor = V <= 8 ? 16 : V == 16 ? 8 : 4;
+constexpr int kRouteCtas = 2 * kAllSms;          // CTAs of a launch besides one for each rank, one wave; bounds the scratch
 constexpr int kEndCtas = 8;                      // one cluster
 constexpr int kClusterRanks = 8;                 // ranks up to which a grid may be one cluster that ends by itself
 
@@ -300,7 +298,7 @@ __global__ void __launch_bounds__(1024) route_end_kernel(const __grid_constant__
 // the other; else each counts the ones in front of it.  (One search of the whole row for each choice took 1090 instructions a row of 256 and 50 us for
 // 32,000 rows, most of it on the half-rate integer pipe.)
 template <int DT, int V, int L, bool VEC>
-__global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_kernel(const __grid_constant__ RouteArgs a) {
+__global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_kernel(const __grid_constant__ RouteArgs a) {
   constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;     // rows of a warp, of the CTA, at a time
   constexpr int kFound = kRows * L * V;
   constexpr int kEnd = W * L * V + end_words(kClusterRanks, W);  // words of the sums and of their end, which reuse the candidates' room
@@ -476,7 +474,7 @@ __device__ __forceinline__ float logit_at(const void* base, unsigned long long a
 // dlogits_j = p_j (c_j - shift) + what the weights' gradient adds to the chosen.  The latter comes through shared memory, where expert e of a row lies at
 // the place that its lane reads without a bank conflict; what was added is set back to zero behind the row.
 template <int DT, int V, int L, bool VEC>
-__global__ void __launch_bounds__(kWarpsFor<V> * 32, kCtasFor<V>) route_backward_kernel(const __grid_constant__ RouteArgs a) {
+__global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_backward_kernel(const __grid_constant__ RouteArgs a) {
   constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;
   __shared__ float extra[kRows][L * V];
   __shared__ unsigned char seen[kRows][L * V];
@@ -603,7 +601,7 @@ int shape_of(int experts) {
   return s;
 }
 int lanes_of(int shape) { return 8 << std::min(shape, 2); }
-int warps_of(int shape) { return shape == 7 ? kRouteWarps / 2 : kRouteWarps; }
+int warps_of(int shape) { return shape <= 5 ? kWarpsFor<8> : shape == 6 ? kWarpsFor<16> : kWarpsFor<32>; }
 size_t rows_at_once(int shape) { return (size_t)warps_of(shape) * (32 / lanes_of(shape)); }
 
 template <int DT, bool VEC>
