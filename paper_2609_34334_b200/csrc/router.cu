@@ -158,9 +158,9 @@ struct ClusterSums {
 };
 
 // Adds the CTAs' sums in a fixed order.  The CTAs of the grid, one cluster, take 32 experts at a time each, a lane each; a CTA's warps share the ranks, and a rank's
-// forward CTAs where there are fewer ranks than warps.  Each CTA puts its parts of the losses into the first one's shared memory, which adds them.
-// shared: end_words(R, warps) words.
-__host__ __device__ constexpr int end_words(int R, int warps) { return (3 + kEndCtas) * kMaxRanks + kMaxRanks + 64 * R + 64 * warps; }
+// forward CTAs where there are fewer ranks than warps; beside its expert a lane reads what one forward CTA left of rows and squares.  Each CTA puts its parts of
+// the losses into the first one's shared memory, which adds them.  shared: end_words(R, warps) words.
+__host__ __device__ constexpr int end_words(int R, int warps) { return (4 + kEndCtas) * kMaxRanks + 64 * R + 66 * warps; }
 template <class Sums>
 __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, float* shared) {
   constexpr int F = Sums::kFlight;
@@ -171,35 +171,10 @@ __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, fl
   float* logs = parts + (kEndCtas + 1) * kMaxRanks;                     // [kMaxRanks]
   float* p_rank = logs + kMaxRanks;                                     // [R][32]
   int* c_rank = reinterpret_cast<int*>(p_rank + 32 * a.R);
-  float* p_part = p_rank + 64 * a.R;                                    // [warps][32]
-  int* c_part = reinterpret_cast<int*>(p_part + 32 * warps);
+  float* p_part = p_rank + 64 * a.R;                                    // [warps][32], then [warps]: squares
+  int* c_part = reinterpret_cast<int*>(p_part + 33 * warps);            // [warps][32], then [warps]: rows
   int split = 1;
   while (split * 2 * a.R <= warps) split *= 2;                          // warps of one rank
-  for (int r = warp; r < a.R; r += warps) {                             // every CTA needs the ranks' rows
-    int n = 0;
-    float z = 0;
-    for (unsigned b0 = a.first[r] + lane; b0 < a.first[r + 1]; b0 += 32 * 4) {
-      int ns[4];
-      float zs[4];
-#pragma unroll
-      for (int u = 0; u < 4; u++) {
-        const unsigned b = b0 + u * 32;
-        ns[u] = b < a.first[r + 1] ? in.count(b, a.experts) : 0;
-        zs[u] = b < a.first[r + 1] ? in.squares(b) : 0.0f;
-      }
-#pragma unroll
-      for (int u = 0; u < 4; u++) {
-        n += ns[u];
-        z += zs[u];
-      }
-    }
-    n = __reduce_add_sync(0xffffffffu, n);
-    z = lanes_sum<32>(z);
-    if (lane == 0) {
-      rows[r] = n;
-      logs[r] = z;
-    }
-  }
   constexpr int kGroups = 2;                                            // of a warp: 64 ranks on 32 warps, kClusterRanks on 4
   float loss[kGroups];                                                  // of group warp + i * warps, in this CTA's experts
 #pragma unroll
@@ -208,17 +183,23 @@ __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, fl
     const int e = e0 + lane;
     for (int r0 = 0; r0 < a.R; r0 += warps / split) {
       const int r = r0 + warp / split;
-      float p = 0;
-      int n = 0;
-      if (r < a.R && e < a.experts) {
+      float p = 0, z = 0;
+      int n = 0, m = 0;
+      if (r < a.R) {
         for (unsigned b0 = a.first[r] + warp % split; b0 < a.first[r + 1]; b0 += F * split) {
           float ps[F];
           int ns[F];
 #pragma unroll
           for (int u = 0; u < F; u++) {
             const unsigned b = b0 + u * split;
-            ps[u] = b < a.first[r + 1] ? in.p(b, e) : 0.0f;
-            ns[u] = b < a.first[r + 1] ? in.count(b, e) : 0;
+            const bool some = b < a.first[r + 1] && e < a.experts;
+            ps[u] = some ? in.p(b, e) : 0.0f;
+            ns[u] = some ? in.count(b, e) : 0;
+          }
+          const unsigned b = b0 + lane * split;
+          if (lane < F && b < a.first[r + 1]) {
+            m += in.count(b, a.experts);
+            z += in.squares(b);
           }
 #pragma unroll
           for (int u = 0; u < F; u++) {
@@ -227,19 +208,31 @@ __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, fl
           }
         }
       }
+      m = __reduce_add_sync(0xffffffffu, m);
+      z = lanes_sum<32>(z);
       if (split > 1) {
         p_part[warp * 32 + lane] = p;
         c_part[warp * 32 + lane] = n;
+        if (lane == 0) {
+          p_part[32 * warps + warp] = z;
+          c_part[32 * warps + warp] = m;
+        }
         __syncthreads();
         if (warp % split == 0 && r < a.R)
           for (int w = 1; w < split; w++) {
             p += p_part[(warp + w) * 32 + lane];
             n += c_part[(warp + w) * 32 + lane];
+            z += p_part[32 * warps + warp + w];
+            m += c_part[32 * warps + warp + w];
           }
       }
       if (warp % split == 0 && r < a.R) {
         p_rank[r * 32 + lane] = p;
         c_rank[r * 32 + lane] = n;
+        if (lane == 0) {
+          rows[r] = m;
+          logs[r] = z;
+        }
         if (e < a.experts) static_cast<int*>(a.dlogits[r])[e] = n;
       }
     }
@@ -257,7 +250,8 @@ __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, fl
         c += c_rank[r * 32 + lane];
         n += rows[r];
       }
-      const double each = n ? 1.0 / (double)n : 0.0, f = (double)c * each * a.per_choice;   // rounded to binary32 once
+      // 1 / n by a step of Newton's iteration from binary32's: off by 2^-44, and what comes of it is rounded to binary32 once
+      const double guess = n ? (double)__frcp_rn((float)n) : 0.0, each = guess * (2.0 - (double)n * guess), f = (double)c * each * a.per_choice;
       if (e < a.experts) a.saved_out[(size_t)g * (a.experts + 1) + e] = (float)(a.balance * f * each);
       loss[i] += n ? (float)(f * each) * p : p;                         // no rows: 0, or NaN
       if (lane == 0) per_row[g] = each;
@@ -278,7 +272,8 @@ __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, fl
   for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
     const int r0 = a.groups > 1 ? g : 0, r1 = a.groups > 1 ? g + 1 : a.R;
     float l = 0.0f, z = 0.0f;
-    for (int c = 0; c < ctas; c++) l += parts[c * kMaxRanks + g];
+#pragma unroll
+    for (int c = 0; c < kEndCtas; c++) l += c < ctas ? parts[c * kMaxRanks + g] : 0.0f;
 #pragma unroll 8
     for (int r = r0; r < r1; r++) z += logs[r];
     a.loss[2 * g] = (float)(a.balance * l);
