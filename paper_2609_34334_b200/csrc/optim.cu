@@ -549,14 +549,17 @@ __device__ __forceinline__ double square_of(const void* p, unsigned long long i)
   return (double)x * (double)x;
 }
 
-__device__ __forceinline__ double cta_sum(double s, double* shared) {   // in a fixed order; valid in thread 0
+__device__ __forceinline__ double warp_sum(double s) {
 #pragma unroll
   for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-  if ((threadIdx.x & 31) == 0) shared[threadIdx.x / 32] = s;
-  __syncthreads();
-  if (threadIdx.x == 0)
-    for (unsigned w = 1; w < blockDim.x / 32; w++) s += shared[w];
   return s;
+}
+__device__ __forceinline__ double cta_sum(double s, double* shared) {   // in a fixed order; valid in the first warp
+  const int lane = threadIdx.x & 31;
+  s = warp_sum(s);
+  if (lane == 0) shared[threadIdx.x / 32] = s;
+  __syncthreads();
+  return threadIdx.x < 32 ? warp_sum(lane < (int)blockDim.x / 32 ? shared[lane] : 0.0) : 0.0;
 }
 
 template <int DT, class Table>
@@ -594,11 +597,16 @@ struct NormEndArgs {
   double max_norm;
   float* out;
 };
-__global__ void __launch_bounds__(kNormThreads) norm_end_kernel(const __grid_constant__ NormEndArgs a) {
-  __shared__ double shared[kNormThreads / 32];
+constexpr int kNormEndThreads = 512;
+__global__ void __launch_bounds__(kNormEndThreads) norm_end_kernel(const __grid_constant__ NormEndArgs a) {
+  __shared__ double shared[kNormEndThreads / 32];
+  constexpr int kEach = (kNormCtas + kNormEndThreads - 1) / kNormEndThreads;
   wait_for_stream();
-  double s = 0;
-  for (int i = threadIdx.x; i < a.n; i += kNormThreads) s += a.partial[i];
+  double x[kEach], s = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; i++) x[i] = (int)threadIdx.x + i * kNormEndThreads < a.n ? __ldcg(a.partial + threadIdx.x + i * kNormEndThreads) : 0.0;
+#pragma unroll
+  for (int i = 0; i < kEach; i++) s += x[i];
   s = cta_sum(s, shared);
   if (threadIdx.x == 0) {
     const double norm = sqrt(s);
@@ -958,7 +966,7 @@ extern "C" hoccl_result_t hoccl_grad_norm(const void* const* grads, const size_t
     if (rows.size() <= 64) CU_TRY(c, norm_launches<NormTableSmall>(rows, 64, (int)dtype, grid, partial, (cudaStream_t)stream));
     else CU_TRY(c, norm_launches<NormTable>(rows, kNormRows, (int)dtype, grid, partial, (cudaStream_t)stream));
     NormEndArgs end{partial, grid, max_norm, out};
-    CU_TRY(c, launch_in_order(reinterpret_cast<const void*>(&norm_end_kernel), 1, kNormThreads, &end, (cudaStream_t)stream));
+    CU_TRY(c, launch_in_order(reinterpret_cast<const void*>(&norm_end_kernel), 1, kNormEndThreads, &end, (cudaStream_t)stream));
   } catch (const std::bad_alloc&) {
     return HOCCL_ERR_INTERNAL;
   }
