@@ -1,8 +1,9 @@
 // The operators of a training step that read gradients: the AdamW step over many tensors, the same step on R ranks with sharded
 // state (reduce-scatter, update, all-gather in one kernel) and the gradient norm.  (The paper has no counterpart.)
 //
-// All three stream: HBM bounds them.  An element of a bf16 weight with a binary32 master and states moves 28 bytes (gradient 2, master, m
-// and v 4 in and 4 out, weight 2 out) and takes some 20 instructions; with 8-bit states 16 bytes and some 70.
+// All three stream.  An element of a bf16 weight with a binary32 master and states moves 28 bytes (gradient 2, master, m and v 4 in and 4 out, weight 2 out) and
+// takes 35 instructions: HBM bounds it (201 M weights 821 us, 6.87 TB/s).  With 8-bit states it moves 16 bytes and takes 70: the issue of
+// instructions bounds it (541 to 570 us, 5.7 to 6.0 TB/s), so its arithmetic goes two numbers an instruction and every step of the rounding is counted.
 // The unit of work is a block of 256 elements, one warp's: the elements that share a scale in 8-bit states, so that a block's
 // largest value is one warp reduction and states of either kind have one shape.  In an aligned, whole block lane l holds elements 8 l .. 8 l + 7 (32-byte
 // accesses of binary32 arrays, 16 of bf16, 8 of codes); in any other one elements l, l + 32, ...  Both run the same arithmetic: alignment changes no bit.
@@ -54,7 +55,8 @@ struct AdamRow {
   float decay;
   unsigned flags;   // bit 0: aligned; the rest: number of the tensor in the caller's table
 };
-// Tensors by value: a launch carries up to 32 (2.4 KB of parameters, 1.2 us of the host's time), 96 (7 KB) or 420 (32 KB, the most there is: 12 us).
+// Tensors by value: a launch carries up to 32 (2.4 KB of parameters; a call takes 2.9 us of the host's time), 96 (7 KB, 3.2 us) or 420 (32 KB, the most there
+// is, 5.0 us).
 template <int N>
 struct AdamTableT {
   int n, pad;
@@ -462,6 +464,8 @@ __global__ void __launch_bounds__(kOptThreads, 32 / kWarps) adamw_kernel(const _
   else tensor_block<GT, W, STATE, WHOLE>(grad, param, a, s, r, keep);
 }
 
+// The gradients of a block are read from every rank at once and its new weights stored to every rank: the reads and writes of an all-reduce, with the state's in
+// between.  13.1 M bf16 weights over 8 ranks: 115 us, 6.3 TB/s (with four of eight gradients in flight and 170 registers 278 us; the pair of collectives alone 211).
 template <int GT, int W, int STATE, Mode MODE>
 __device__ __forceinline__ void sharded_block(const ShardedArgs& args, const AdamScalars& s, const Rates& r, int c, unsigned long long lo, const Place& a) {
   // the ring's order: c + 1, c + 2, ..., c; the gradients of kFlight ranks in flight at a time, as they lie in memory
@@ -526,7 +530,7 @@ using NormTableSmall = NormTableT<64>;
 using NormTable = NormTableT<kNormRows>;
 static_assert(sizeof(NormTable) <= 32764, "kernel parameters");
 
-// Squares in binary64: the square of any binary32 number is there, and a long sum keeps its bits.
+// 201 M bf16 gradients: 63 us, 6.4 TB/s.  Squares in binary64: the square of any binary32 number is there, and a long sum keeps its bits.
 template <int DT>
 __device__ __forceinline__ double squares(uint4 r) {
   float x[8];

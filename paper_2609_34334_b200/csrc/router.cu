@@ -4,6 +4,8 @@
 // A row of logits is held by L lanes with V logits each, in registers, for all that is done with it: one read of the logits, no second pass.  Sums over
 // the tokens (the probability of each expert, how often it was chosen) stay in a lane's registers and the CTA's shared memory until the CTA has done its rows;
 // its sums then go to scratch and one cluster of CTAs adds them in a fixed order, so that the same call gives the same bits.
+// Both directions are bound by the issue of instructions and the latency of steps that depend on each other, not by HBM: 32,000 rows of 256 binary32 logits, topk 8, take
+// 26 us forward (35.6 MB, 5.4 us at the copy rate; 450 instructions a row) and 16.4 to 17.8 us backward (69 MB, 10.5 us; 340).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
@@ -23,7 +25,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kMaxExperts = 1024, kMaxTopk = 32;
-// Warps of a CTA: many, so that few CTAs leave sums behind (32,000 rows of 256 experts: 28 us with 8, 2x with 16), as far as the candidates' room allows.
+// Warps of a CTA: many, so that few CTAs leave sums behind (32,000 rows of 256 experts: 28.4 us with 8, 25.8 with 16), as far as the candidates' room allows.
 template <int V>
 constexpr int kWarpsFor = V <= 8 ? 16 : V == 16 ? 8 : 4;
 constexpr int kRouteCtas = 2 * kAllSms;          // CTAs of a launch besides one for each rank, one wave; bounds the scratch
@@ -291,7 +293,7 @@ __global__ void __launch_bounds__(1024) route_end_kernel(const __grid_constant__
 // The topk largest of a row without a pass over it for each: the topk-th largest of the lanes' own largest logits is a bar that at least topk logits reach, and
 // few more do (a dozen for 8 of 256); those are collected.  Where a lane can hold each of them and no two are alike, a maximum over the warp finds one after
 // the other; else each counts the ones in front of it.  (One search of the whole row for each choice took 1090 instructions a row of 256 and 50 us for
-// 32,000 rows, most of it on the half-rate integer pipe.)
+// 32,000 rows, most of it on the half-rate integer pipe; this form takes 23 us, 6 of them for ranking and writing, 5.3 for the bar and the collecting.)
 template <int DT, int V, int L, bool VEC>
 __global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_kernel(const __grid_constant__ RouteArgs a) {
   constexpr int W = kWarpsFor<V>, G = 32 / L, kRows = W * G;     // rows of a warp, of the CTA, at a time
