@@ -755,7 +755,7 @@ struct hoccl_adamw_plan {
 
 namespace {
 
-constexpr size_t kMaxTensorElements = 1ull << 39;   // 2^28 tiles; with those of 64 ranks' chunks a grid's 2^31 hold them
+constexpr size_t kMaxTensorElements = 1ull << 39;   // 2^29 tiles; with those of 64 ranks' chunks a grid holds them
 
 template <class Table>
 void append_table(const std::vector<AdamRow>& rows, size_t from, size_t n, std::vector<Table>* out) {

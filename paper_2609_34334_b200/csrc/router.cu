@@ -279,7 +279,7 @@ __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, fl
 #pragma unroll 8
     for (int r = r0; r < r1; r++) z += logs[r];
     a.loss[2 * g] = (float)(a.balance * l);
-    a.loss[2 * g + 1] = (float)(a.z * per_row[g] * z);
+    a.loss[2 * g + 1] = a.z == 0.0 ? 0.0f : (float)(a.z * per_row[g] * z);   // (the sum of squares may be infinite)
     a.saved_out[(size_t)g * (a.experts + 1) + a.experts] = (float)(2.0 * a.z * per_row[g]);
   }
 }

@@ -330,6 +330,18 @@ def test_rates_on_the_device_in_a_captured_step(comm):
             s.dev[k].copy_(ref.dev[k])
 
 
+def test_an_empty_plan_and_shared_gradients(comm):
+    comm.adamw(hb.AdamTensors([], [], [], [], "fp32", "fp32"), 1e-3, 1)
+    g = torch.randn(300, device="cuda")
+    z = lambda: [torch.zeros(300, device="cuda") for _ in range(2)]  # noqa: E731
+    p, m, v = z(), z(), z()
+    t = hb.AdamTensors(p, [g, g], m, v, "fp32", "fp32")
+    comm.adamw(t, 1e-3, 1)
+    t.destroy()
+    torch.cuda.synchronize()
+    assert p[0].any() and all(torch.equal(a[0], a[1]) for a in (p, m, v))
+
+
 def test_other_streams_and_repeated_calls(comm):
     s, ref = (Set([200_000], "bf16", True, "bf16", "fp32") for _ in range(2))
     side = torch.cuda.Stream()

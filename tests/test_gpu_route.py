@@ -111,6 +111,59 @@ def test_nothing_open_anywhere():
     assert not c.counts.any() and not c.loss[:-1].any() and not c.saved[:-1].any()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("E", [8, 61, 256])
+def test_the_lowest_number_is_a_logit(E, dtype):
+    """Rows and entries masked with the type's lowest number, not with -infinity."""
+    low = torch.finfo(DT[dtype]).min
+    x = torch.randn(6, E, device="cuda").to(DT[dtype])
+    x[0] = low
+    x[1, 1:] = low
+    x[2, ::2] = low
+    c = Call(1, [6], E, 3, dtype, False, False, [x])
+    c.comm.route(c.x, c.tokens, E, 3, dtype, c.indices, c.weights, list(c.counts), c.loss, c.saved, balance_coef=BAL, z_coef=0.0, normalize=False)
+    i, w, p, _, _, rel = route(x.cpu().double(), 3, False)
+    assert torch.equal(c.indices[0][:6].cpu().long(), i) and int(c.counts[0, E]) == 6
+    # the bound of each weight's own distance from the row's largest; below the least normal number it is 0
+    assert ((c.weights[0][:6].cpu().double() - w).abs() <= 2 * torch.gather(rel, 1, i) * w + 2.0 ** -126).all()
+    assert float(c.loss[1]) == 0.0 and math.isfinite(float(c.loss[0]))
+    out = [torch.zeros(7, E, dtype=DT[dtype], device="cuda")]
+    backward(c, [torch.ones(7, 3, device="cuda")], None, out)
+    assert out[0].isfinite().all()
+
+
+def test_small_grids_captured_and_repeated():
+    """The form that ends inside one cluster: captured, replayed on new logits, and the same bits as an eager call; one communicator for several shapes."""
+    comm = hb.Comm(8, 0)
+    n = max(hb.route_scratch_bytes(8, 64, E) for E in (8, 64, 256, 1024))
+    scratch = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    comm.set_scratch(scratch)
+    side = torch.cuda.Stream()
+    for E, K, T in ((8, 2, 5), (64, 6, 16), (256, 8, 1), (1024, 32, 3), (64, 6, 64), (64, 6, 0)):
+        calls = []
+        for _ in range(2):
+            c = Call(8, [T] * 8, E, K, "bf16", True, False, None)
+            c.comm = comm
+            c.x = make(8, [max(T, 1)] * 8, E, "bf16")
+            calls.append(c)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            calls[0].forward(stream=side)
+        for _ in range(3):
+            for a, b in zip(calls[0].x, calls[1].x):
+                a.add_(torch.randn_like(a))
+                b.copy_(a)
+            graph.replay()
+            calls[1].forward()
+            torch.cuda.synchronize()
+            for name in ("counts", "loss", "saved"):
+                assert torch.equal(getattr(calls[0], name), getattr(calls[1], name)), (E, name)
+            for name in ("indices", "weights"):
+                assert all(torch.equal(a, b) for a, b in zip(getattr(calls[0], name), getattr(calls[1], name))), (E, name)
+    comm.destroy()
+
+
 @pytest.mark.parametrize("E", [8, 61, 256])
 def test_nan_is_not_chosen_and_shows(E):
     x = make(1, [40], E, "fp32", pad=0, closed=0)
@@ -189,6 +242,23 @@ def test_backward(R, tokens, E, K, dtype):
             backward(c, a, b, out)
             check_backward(c, a, b, out)
         assert all((o[-1] == 5).all() for o in out)
+
+
+@pytest.mark.parametrize("normalize", [True, False])
+def test_gradients_beside_no_choice_are_not_read(normalize):
+    """Rows of padding and rows with fewer open experts than choices: what lies in dweights beside -1 may be anything."""
+    E, K, T = 16, 4, 30
+    x = make(1, [T], E, "fp32", pad=0.3, closed=0.8)
+    c = Call(1, [T], E, K, "fp32", normalize, False, x).forward()
+    dw = torch.randn(T, K, device="cuda")
+    none = c.indices[0][:T] < 0
+    assert none.any() and not none.all()
+    bad = torch.where(none, math.nan, dw)
+    out = [torch.zeros(T, E, device="cuda")]
+    backward(c, [bad], None, out)
+    check_backward(c, [torch.where(none, 0.0, dw)], None, out)
+    closed = (x[0] == -math.inf).all(1)
+    assert closed.any() and not out[0][closed].any()
 
 
 @pytest.mark.parametrize("E,ld,dld,off", [(64, 72, 80, 0), (64, 65, 64, 0), (61, 100, 61, 3), (256, 256, 264, 0), (8, 9, 11, 2)])
