@@ -465,7 +465,8 @@ __global__ void __launch_bounds__(kOptThreads, 32 / kWarps) adamw_kernel(const _
 }
 
 // The gradients of a block are read from every rank at once and its new weights stored to every rank: the reads and writes of an all-reduce, with the state's in
-// between.  13.1 M bf16 weights over 8 ranks: 115 us, 6.3 TB/s (with four of eight gradients in flight and 170 registers 278 us; the pair of collectives alone 211).
+// between.  13.1 M bf16 weights over 8 ranks: 117 us, 6.3 TB/s (with four of eight gradients in flight and 170 registers 278 us; the pair of collectives alone 211);
+// one weight more, which puts chunks off 32 bytes, 139 us (64 registers; 146 with 80, 175 with 128 and all eight gradients in flight).
 template <int GT, int W, int STATE, Mode MODE>
 __device__ __forceinline__ void sharded_block(const ShardedArgs& args, const AdamScalars& s, const Rates& r, int c, unsigned long long lo, const Place& a) {
   // the ring's order: c + 1, c + 2, ..., c; the gradients of kFlight ranks in flight at a time, as they lie in memory
@@ -497,7 +498,7 @@ __device__ __forceinline__ void sharded_block(const ShardedArgs& args, const Ada
 }
 
 template <int GT, int W, int STATE>
-__global__ void __launch_bounds__(kOptThreads, 24 / kWarps) sharded_adamw_kernel(const __grid_constant__ ShardedArgs args, const __grid_constant__ AdamScalars s) {
+__global__ void __launch_bounds__(kOptThreads, 32 / kWarps) sharded_adamw_kernel(const __grid_constant__ ShardedArgs args, const __grid_constant__ AdamScalars s) {
   wait_for_stream();
   const Rates r = read_rates(s);
   if (r.skip) return;
