@@ -605,7 +605,7 @@ hoccl_result_t hoccl_grad_norm(const void* const* grads, const size_t* counts, i
  * Router of an expert-parallel layer.  Rank r has tokens[r] rows of `experts` logits (dtype; `ld` elements from row to row, ld >= experts) and gets, row by row,
  *   indices[r][k], k < topk: the experts of the topk largest logits, largest first, of equal ones the lowest index first; -1 where fewer than topk
  *                  logits are above -infinity (a masked expert; a row with none is padding: it chooses nothing and counts nowhere);
- *   weights[r][k]: their probabilities p = softmax(row), divided by their sum if `normalize`; 0 beside -1;
+ *   weights[r][k]: their probabilities p = softmax(row), divided by their sum if `normalize`; 0 beside -1, and where p is below the least normal binary32 number;
  * and counts[r], experts + 1 ints: how often each expert was chosen, then the number of rows that chose any: what the counts of an hoccl_alltoallv are made of.
  * loss (two floats for each group) and saved (experts + 1 floats for each group): over the n such rows of all ranks (one group), or of each rank by itself
  * (`per_rank`: R groups), with f_e = count of e / (topk * n) and P_e = the rows' sum of p_e / n:
