@@ -589,23 +589,34 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_backw
 
 // ---------------------------------------------------------------- host
 
-// Shapes: as many lanes as there are experts up to 32, from 8 on; then 2, 4, ... 32 logits a lane.  topk is at most the experts and at most 32, so a lane
-// holds one of a row's chosen.
-constexpr int kShapes = 8;
-int shape_of(int experts) {
-  int s = 0;
-  while ((8 << s) < experts) s++;
-  return s;
+// Shapes: 8, 16 or 32 lanes a row with 1, 2, 4 or 8 logits each, 32 lanes with 16 or 32.  topk is at most the lanes, so a lane holds one of a row's chosen.
+// Fewer lanes put more rows into a warp, which then share what an instruction does for a row beside its logits; more lanes end a row sooner.  us for 8 ranks
+// of n rows, forward and backward, with 32 lanes and with the fewest: 32 experts, topk 4, n = 16 5.9 + 2.3 and 6.1 + 2.5, n = 512 9.6 + 2.9 and 9.5 + 2.8,
+// n = 8192 27.5 + 18.4 and 17.8 + 8.7; 128 experts, topk 8, n = 16 6.8 + 2.7 and 7.8 + 3.0, n = 512 11.5 + 3.5 and 11.7 + 3.4, n = 8192 40.3 + 24.0 and 35.6 + 15.4.
+constexpr int kShapes = 14;
+constexpr unsigned long long kFewRows = 4096;   // of all ranks
+int shape_with(int lanes, int experts) {        // -1: none
+  int log_v = 0;
+  while ((lanes << log_v) < experts) log_v++;
+  if (lanes == 32) return 8 + log_v;
+  return log_v > 3 ? -1 : (lanes == 8 ? 0 : 4) + log_v;
 }
-int lanes_of(int shape) { return 8 << std::min(shape, 2); }
-int warps_of(int shape) { return shape <= 5 ? kWarpsFor<8> : shape == 6 ? kWarpsFor<16> : kWarpsFor<32>; }
+int lanes_of(int shape) { return shape < 4 ? 8 : shape < 8 ? 16 : 32; }
+int warps_of(int shape) { return shape <= 11 ? kWarpsFor<8> : shape == 12 ? kWarpsFor<16> : kWarpsFor<32>; }
 size_t rows_at_once(int shape) { return (size_t)warps_of(shape) * (32 / lanes_of(shape)); }
+// The shape with the fewest lanes, of which there are at least `least`.
+int compact_shape(int experts, int least) {
+  for (int lanes = 8; lanes < 32; lanes *= 2)
+    if (lanes >= least && shape_with(lanes, experts) >= 0) return shape_with(lanes, experts);
+  return shape_with(32, experts);
+}
 
 template <int DT, bool VEC>
 const void* route_entry_of(int shape, bool backward) {
   // a lane's logits are at least a vector of 16 bytes
 #define ROW(V, L) {reinterpret_cast<const void*>(&route_kernel<DT, V, L, (VEC && V >= Traits<DT>::VE)>), reinterpret_cast<const void*>(&route_backward_kernel<DT, V, L, (VEC && V >= Traits<DT>::VE)>)}
-  static const void* const fns[kShapes][2] = {ROW(1, 8), ROW(1, 16), ROW(1, 32), ROW(2, 32), ROW(4, 32), ROW(8, 32), ROW(16, 32), ROW(32, 32)};
+  static const void* const fns[kShapes][2] = {ROW(1, 8),  ROW(2, 8),  ROW(4, 8),  ROW(8, 8),  ROW(1, 16), ROW(2, 16),  ROW(4, 16),
+                                              ROW(8, 16), ROW(1, 32), ROW(2, 32), ROW(4, 32), ROW(8, 32), ROW(16, 32), ROW(32, 32)};
 #undef ROW
   return fns[shape][backward];
 }
@@ -644,10 +655,15 @@ hoccl_result_t check_config(const hoccl_comm* c, const hoccl_route_config_t* f, 
   return HOCCL_OK;
 }
 
-// Rows of one CTA and the ranks' first CTAs: as many CTAs as `most` at most, besides one for each rank, and no fewer rows in one than its warps hold.
-unsigned share_rows(const size_t* tokens, int R, int shape, unsigned most, unsigned* rows_per_cta, unsigned* first) {
+unsigned long long rows_of(const size_t* tokens, int R) {
   unsigned long long all = 0;
   for (int r = 0; r < R; r++) all += tokens[r];
+  return all;
+}
+
+// Rows of one CTA and the ranks' first CTAs: as many CTAs as `most` at most, besides one for each rank, and no fewer rows in one than its warps hold.
+unsigned share_rows(const size_t* tokens, int R, int shape, unsigned most, unsigned* rows_per_cta, unsigned* first) {
+  const unsigned long long all = rows_of(tokens, R);
   const unsigned long long at_once = rows_at_once(shape);
   unsigned long long per = (all + most - 1) / most;
   per = std::max((per + at_once - 1) / at_once, 1ull) * at_once;
@@ -687,7 +703,7 @@ extern "C" {
 
 size_t hoccl_route_scratch_bytes(int R, size_t max_tokens, int experts) {
   if (R < 1 || R > kMaxRanks || experts < 1 || experts > kMaxExperts) return 0;
-  const size_t at_once = rows_at_once(shape_of(experts));
+  const size_t at_once = rows_at_once(shape_with(32, experts));   // the fewest of the shapes it may take
   const size_t ctas = std::min((size_t)R * ((max_tokens + at_once - 1) / at_once), (size_t)kRouteCtas + R);
   return (ctas * (2 * (size_t)experts + 2) * sizeof(float) + 255) / 256 * 256;
 }
@@ -700,7 +716,7 @@ hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* t
   if (!indices || !weights || !counts || !loss || !saved || !aligned_to(loss, 4) || !aligned_to(saved, 4)) return HOCCL_ERR_INVALID_ARG;
   if (!std::isfinite(f->balance_coef) || !std::isfinite(f->z_coef)) return HOCCL_ERR_INVALID_ARG;
   const size_t e = dtype_size((int)f->dtype);
-  const int shape = shape_of(f->experts), groups = f->per_rank ? c->R : 1;
+  const int groups = f->per_rank ? c->R : 1;
   RouteArgs a = {};
   a.R = c->R;
   a.experts = f->experts;
@@ -735,10 +751,17 @@ hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* t
   } catch (const std::bad_alloc&) {
     return HOCCL_ERR_INTERNAL;
   }
-  unsigned grid = share_rows(tokens, c->R, shape, kRouteCtas, &a.rows_per_cta, a.first);
+  // the bar of the choice is the topk-th of as many numbers as there are lanes: few of them would let many logits over it
+  const int wide = shape_with(32, f->experts), compact = compact_shape(f->experts, 2 * f->topk);
+  int shape = wide;
+  unsigned grid = share_rows(tokens, c->R, wide, kRouteCtas, &a.rows_per_cta, a.first);
   const size_t need = (size_t)grid * (2 * (size_t)f->experts + 2) * sizeof(float);
-  const bool one_cluster = grid && share_in_cluster(tokens, c->R, shape, &a.rows_per_cta, a.first);   // ends by itself
-  if (one_cluster) grid = a.first[c->R];
+  bool one_cluster = grid && share_in_cluster(tokens, c->R, wide, &a.rows_per_cta, a.first);   // ends by itself
+  if (grid && !one_cluster && compact != wide) {
+    one_cluster = share_in_cluster(tokens, c->R, compact, &a.rows_per_cta, a.first);
+    if (one_cluster || rows_of(tokens, c->R) > kFewRows) shape = compact;
+  }
+  grid = one_cluster ? a.first[c->R] : share_rows(tokens, c->R, shape, kRouteCtas, &a.rows_per_cta, a.first);
   if (need && (!c->scratch || c->scratch_bytes < need)) return HOCCL_ERR_SCRATCH;
   a.partial = one_cluster ? nullptr : static_cast<float*>(c->scratch);
   c->stats = hoccl_stats_t{};
@@ -763,7 +786,7 @@ hoccl_result_t hoccl_route_backward(const void* const* logits, size_t ld, const 
   if (rc != HOCCL_OK) return rc;
   if ((dweights && !indices) || !saved || !dlogits || !aligned_to(saved, 4) || !aligned_to(dloss, 4) || dld < (size_t)f->experts || dld > 1ull << 31) return HOCCL_ERR_INVALID_ARG;
   const size_t e = dtype_size((int)f->dtype);
-  const int shape = shape_of(f->experts), groups = f->per_rank ? c->R : 1;
+  const int groups = f->per_rank ? c->R : 1;
   RouteArgs a = {};
   a.R = c->R;
   a.experts = f->experts;
@@ -801,6 +824,7 @@ hoccl_result_t hoccl_route_backward(const void* const* logits, size_t ld, const 
     return HOCCL_ERR_INTERNAL;
   }
   c->stats = hoccl_stats_t{};
+  const int shape = rows_of(tokens, c->R) > kFewRows ? compact_shape(f->experts, f->topk) : shape_with(32, f->experts);
   const unsigned grid = share_rows(tokens, c->R, shape, kRouteCtas, &a.rows_per_cta, a.first);
   if (!grid) return HOCCL_OK;
   DeviceScope scope(c->device);

@@ -72,7 +72,9 @@ class Call:
 
 
 SHAPES = [(1, [1], 1, 1), (3, [300, 1, 77], 2, 2), (2, [70, 9], 9, 9), (8, [5] * 8, 32, 31), (2, [3, 5], 4, 2), (3, [17, 0, 40], 8, 8), (2, [100, 33], 16, 16), (4, [64, 1, 63, 65], 61, 3), (2, [257, 300], 64, 6), (2, [50, 20], 96, 4), (8, [40] * 8, 128, 8),
-          (2, [100, 77], 256, 8), (1, [130], 257, 5), (2, [33, 30], 512, 32), (1, [19], 1000, 7), (2, [9, 8], 1024, 1), (64, [3] * 64, 60, 2), (2, [5000, 4000], 32, 2)]
+          (2, [100, 77], 256, 8), (1, [130], 257, 5), (2, [33, 30], 512, 32), (1, [19], 1000, 7), (2, [9, 8], 1024, 1), (64, [3] * 64, 60, 2), (2, [5000, 4000], 32, 2),
+          (1, [4200], 8, 8), (1, [4200], 16, 3), (1, [4200], 61, 3), (2, [4000, 201], 64, 6), (1, [4200], 100, 8), (1, [4200], 30, 14), (1, [4200], 14, 8), (1, [4200], 128, 16), (1, [4200], 5, 1),
+          (8, [100] * 8, 32, 4), (8, [60] * 8, 64, 2), (1, [5000], 128, 2), (1, [5000], 256, 2)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
