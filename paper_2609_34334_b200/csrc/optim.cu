@@ -53,7 +53,7 @@ struct AdamRow {
   float *master, *m_scale, *v_scale;
   unsigned long long n;
   float decay;
-  unsigned flags;   // bit 0: aligned; the rest: number of the tensor in the caller's table
+  unsigned flags;   // bit 0: aligned for eight elements at a time; the rest: number of the tensor in the caller's table
 };
 // Tensors by value: a launch carries up to 32 (2.4 KB of parameters; a call takes 2.9 us of the host's time), 96 (7 KB, 3.2 us) or 420 (32 KB, the most there
 // is, 5.0 us).
@@ -73,7 +73,7 @@ struct ShardedArgs {
   float decay;
   unsigned per_rank;             // tiles of a full chunk: a CTA each
   unsigned long long count, q;
-  unsigned long long aligned;    // bit c: chunk c
+  unsigned long long aligned, paired;   // bit c: chunk c, for eight and for two elements at a time
   const void* grad[kMaxRanks];
   void* param[kMaxRanks];
   void *m[kMaxRanks], *v[kMaxRanks];
@@ -157,12 +157,15 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either 
   return r;
 }
 
-// How a block is read and written: element by element within the array's end, element by element all of it, or in aligned vectors.
-enum Mode { ENDS, WHOLE, VECTORS };
+// How a block is read and written: element by element within the array's end, element by element all of it, two elements at a time (arrays that start on two
+// elements' boundary; the sharded step alone: half as many accesses of every rank's arrays, where the plain step gains nothing), or eight (on 8 elements').
+enum Mode { ENDS, WHOLE, PAIRS, VECTORS };
 // Where a thread's eight elements lie in its tile, and whether they exist where `left` elements do.
 template <Mode MODE>
 __device__ __forceinline__ unsigned element(int i) {
-  return MODE == VECTORS ? threadIdx.x * 8 + i : (threadIdx.x & ~31u) * 8 + i * 32 + (threadIdx.x & 31);
+  if (MODE == VECTORS) return threadIdx.x * 8 + i;
+  const unsigned warp = (threadIdx.x & ~31u) * 8, lane = threadIdx.x & 31;
+  return MODE == PAIRS ? warp + i / 2 * 64 + lane * 2 + i % 2 : warp + i * 32 + lane;
 }
 template <Mode MODE>
 __device__ __forceinline__ bool exists(int i, unsigned left) {
@@ -176,6 +179,13 @@ __device__ __forceinline__ void load_floats(const void* base, unsigned left, flo
     const float* p = static_cast<const float*>(base);
     if (MODE == VECTORS) {
       load8(p + threadIdx.x * 8, x);
+    } else if (MODE == PAIRS) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const float2 r = __ldcs(reinterpret_cast<const float2*>(p + element<MODE>(i)));
+        x[i] = r.x;
+        x[i + 1] = r.y;
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++) x[i] = exists<MODE>(i, left) ? __ldcs(p + element<MODE>(i)) : 0.0f;
@@ -184,6 +194,13 @@ __device__ __forceinline__ void load_floats(const void* base, unsigned left, flo
     const unsigned short* p = static_cast<const unsigned short*>(base);
     if (MODE == VECTORS) {
       widen8(__ldcs(reinterpret_cast<const uint4*>(p) + threadIdx.x), x);
+    } else if (MODE == PAIRS) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const unsigned r = __ldcs(reinterpret_cast<const unsigned*>(p + element<MODE>(i)));
+        x[i] = __uint_as_float(r << 16);
+        x[i + 1] = __uint_as_float(r & 0xffff0000u);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++) x[i] = exists<MODE>(i, left) ? __uint_as_float((unsigned)__ldcs(p + element<MODE>(i)) << 16) : 0.0f;
@@ -201,6 +218,15 @@ struct Raw {
   }
 };
 template <>
+struct Raw<1, PAIRS> {
+  unsigned r[4];
+  __device__ __forceinline__ void load(const void* base, unsigned) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) r[i] = __ldcs(reinterpret_cast<const unsigned*>(static_cast<const unsigned short*>(base) + element<PAIRS>(2 * i)));
+  }
+  __device__ __forceinline__ void widen(float* y) const { widen8(make_uint4(r[0], r[1], r[2], r[3]), y); }
+};
+template <>
 struct Raw<1, VECTORS> {
   uint4 r;
   __device__ __forceinline__ void load(const void* base, unsigned) { r = __ldcs(static_cast<const uint4*>(base) + threadIdx.x); }
@@ -212,6 +238,9 @@ __device__ __forceinline__ void store_floats(void* base, unsigned left, const fl
     float* p = static_cast<float*>(base);
     if (MODE == VECTORS) {
       store8(p + threadIdx.x * 8, x);
+    } else if (MODE == PAIRS) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) __stcs(reinterpret_cast<float2*>(p + element<MODE>(i)), make_float2(x[i], x[i + 1]));
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++)
@@ -221,6 +250,9 @@ __device__ __forceinline__ void store_floats(void* base, unsigned left, const fl
     unsigned short* p = static_cast<unsigned short*>(base);
     if (MODE == VECTORS) {
       __stcs(reinterpret_cast<uint4*>(p) + threadIdx.x, make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])));
+    } else if (MODE == PAIRS) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) __stcs(reinterpret_cast<unsigned*>(p + element<MODE>(i)), pack_bf16(x[i], x[i + 1]));
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++)
@@ -264,6 +296,9 @@ __device__ __forceinline__ void load_codes(const void* base, unsigned left, floa
     pair[1] = (unsigned short)(r.x >> 16);
     pair[2] = (unsigned short)r.y;
     pair[3] = (unsigned short)(r.y >> 16);
+  } else if (MODE == PAIRS) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) pair[i] = __ldcs(reinterpret_cast<const unsigned short*>(p + element<MODE>(2 * i)));
   } else {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
@@ -322,6 +357,9 @@ __device__ __forceinline__ void store_codes(void* base, float* scales, unsigned 
   unsigned char* p = static_cast<unsigned char*>(base);
   if (MODE == VECTORS) {
     __stcs(reinterpret_cast<uint2*>(p) + threadIdx.x, make_uint2(pair[0] | (unsigned)pair[1] << 16, pair[2] | (unsigned)pair[3] << 16));
+  } else if (MODE == PAIRS) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) __stcs(reinterpret_cast<unsigned short*>(p + element<MODE>(2 * i)), pair[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; i++)
@@ -466,11 +504,12 @@ __global__ void __launch_bounds__(kOptThreads, 32 / kWarps) adamw_kernel(const _
 
 // The gradients of a block are read from every rank at once and its new weights stored to every rank: the reads and writes of an all-reduce, with the state's in
 // between.  13.1 M bf16 weights over 8 ranks: 117 us, 6.3 TB/s (with four of eight gradients in flight and 170 registers 278 us; the pair of collectives alone 211);
-// one weight more, which puts chunks off 32 bytes, 139 us (64 registers; 146 with 80, 175 with 128 and all eight gradients in flight).
+// one weight more, which puts chunks off 32 bytes, 129 us (two elements at a time in every other chunk, one in the rest; 139 with one in all; 146 with 80 registers
+// instead of 64, 175 with 128 and all eight gradients in flight).
 template <int GT, int W, int STATE, Mode MODE>
 __device__ __forceinline__ void sharded_block(const ShardedArgs& args, const AdamScalars& s, const Rates& r, int c, unsigned long long lo, const Place& a) {
   // the ring's order: c + 1, c + 2, ..., c; the gradients of kFlight ranks in flight at a time, as they lie in memory
-  constexpr int kFlight = MODE != VECTORS ? 2 : GT == 1 ? 8 : 4;
+  constexpr int kFlight = MODE < PAIRS ? 2 : GT == 0 ? 4 : MODE == PAIRS ? 4 : 8;
   float g[8];
   int from = c;
   for (int j0 = 0; j0 < args.R; j0 += kFlight) {
@@ -509,6 +548,7 @@ __global__ void __launch_bounds__(kOptThreads, 32 / kWarps) sharded_adamw_kernel
   const Place a = place_of(args.m[c], args.v[c], args.master[c], args.m_scale[c], args.v_scale[c], n, at, W, STATE, r.seed, (unsigned)c);
   if (here + kBlock > a.left) sharded_block<GT, W, STATE, ENDS>(args, s, r, c, lo + at, a);
   else if (args.aligned >> c & 1) sharded_block<GT, W, STATE, VECTORS>(args, s, r, c, lo + at, a);
+  else if (args.paired >> c & 1) sharded_block<GT, W, STATE, PAIRS>(args, s, r, c, lo + at, a);
   else sharded_block<GT, W, STATE, WHOLE>(args, s, r, c, lo + at, a);
 }
 
@@ -710,11 +750,14 @@ bool regions_clash(std::vector<Region>* regions) {
   return false;
 }
 
-// Checks one tensor's (shard's) state and adds its regions; *aligned is cleared if an array does not start on an access of eight elements.
-bool state_fits(const void* m, const void* v, const float* master, const float* ms, const float* vs, size_t n, int state, std::vector<Region>* regions, bool* aligned) {
+// What a set of arrays shares: bit 0 if all start on an access of eight elements, bit 1 of two.
+unsigned phase_of(const void* p, size_t e) { return (aligned_to(p, 8 * e) ? 1u : 0u) | (aligned_to(p, 2 * e) ? 2u : 0u); }
+
+// Checks one tensor's (shard's) state and adds its regions; *phase loses what its arrays do not have.
+bool state_fits(const void* m, const void* v, const float* master, const float* ms, const float* vs, size_t n, int state, std::vector<Region>* regions, unsigned* phase) {
   const size_t e = state == HOCCL_STATE_FLOAT32 ? 4 : 1;
   if (!m || !v || !aligned_to(m, e) || !aligned_to(v, e) || !aligned_to(master, 4)) return false;
-  *aligned = *aligned && aligned_to(m, 8 * e) && aligned_to(v, 8 * e) && aligned_to(master, 32);
+  *phase &= phase_of(m, e) & phase_of(v, e) & phase_of(master, 4);
   regions->push_back({(const char*)m, n * e, true});
   regions->push_back({(const char*)v, n * e, true});
   if (master) regions->push_back({(const char*)master, n * 4, true});
@@ -781,12 +824,12 @@ hoccl_result_t make_plan(hoccl_adamw_plan_t* out, const hoccl_adamw_tensor_t* te
     if (t.count == 0) continue;
     if (t.count > kMaxTensorElements || !t.param || !t.grad || !aligned_to(t.param, pe) || !aligned_to(t.grad, ge) || !std::isfinite(t.weight_decay)) return HOCCL_ERR_INVALID_ARG;
     (t.master ? with : without) = true;
-    bool aligned = aligned_to(t.param, 8 * pe) && aligned_to(t.grad, 8 * ge);
-    if (!state_fits(t.exp_avg, t.exp_avg_sq, t.master, t.exp_avg_scale, t.exp_avg_sq_scale, t.count, state, &regions, &aligned)) return HOCCL_ERR_INVALID_ARG;
+    unsigned phase = phase_of(t.param, pe) & phase_of(t.grad, ge);
+    if (!state_fits(t.exp_avg, t.exp_avg_sq, t.master, t.exp_avg_scale, t.exp_avg_sq_scale, t.count, state, &regions, &phase)) return HOCCL_ERR_INVALID_ARG;
     regions.push_back({(const char*)t.param, t.count * pe, true});
     regions.push_back({(const char*)t.grad, t.count * ge, false});
     rows.push_back(AdamRow{t.param, t.exp_avg, t.exp_avg_sq, t.grad, t.master, t.exp_avg_scale, t.exp_avg_sq_scale, (unsigned long long)t.count, t.weight_decay,
-                           (unsigned)k << 1 | (aligned ? 1u : 0u)});
+                           (unsigned)k << 1 | (phase & 1)});
   }
   if (with && without) return HOCCL_ERR_INVALID_ARG;
   if (with && param_dtype != HOCCL_BFLOAT16) return HOCCL_ERR_UNSUPPORTED;
@@ -900,10 +943,11 @@ hoccl_result_t hoccl_sharded_adamw(const void* const* grads, void* const* params
       a.master[r] = master ? master[r] : nullptr;
       a.m_scale[r] = eight ? exp_avg_scale[r] : nullptr;
       a.v_scale[r] = eight ? exp_avg_sq_scale[r] : nullptr;
-      bool aligned = true;
-      if ((master && !master[r]) || !state_fits(a.m[r], a.v[r], a.master[r], a.m_scale[r], a.v_scale[r], n, (int)state, &regions, &aligned)) return HOCCL_ERR_INVALID_ARG;
-      for (int k = 0; k < c->R; k++) aligned = aligned && aligned_to((const char*)grads[k] + lo * ge, 8 * ge) && aligned_to((const char*)params[k] + lo * pe, 8 * pe);
-      if (aligned) a.aligned |= 1ull << r;
+      unsigned phase = 3;
+      if ((master && !master[r]) || !state_fits(a.m[r], a.v[r], a.master[r], a.m_scale[r], a.v_scale[r], n, (int)state, &regions, &phase)) return HOCCL_ERR_INVALID_ARG;
+      for (int k = 0; k < c->R; k++) phase &= phase_of((const char*)grads[k] + lo * ge, ge) & phase_of((const char*)params[k] + lo * pe, pe);
+      if (phase & 1) a.aligned |= 1ull << r;
+      if (phase & 2) a.paired |= 1ull << r;
     }
     if (regions_clash(&regions)) return HOCCL_ERR_INVALID_ARG;
   } catch (const std::bad_alloc&) {
