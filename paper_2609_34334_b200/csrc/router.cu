@@ -286,6 +286,7 @@ __device__ __forceinline__ void route_end(const RouteArgs& a, const Sums& in, fl
 
 __global__ void __launch_bounds__(1024) route_end_kernel(const __grid_constant__ RouteArgs a) {
   __shared__ __align__(16) float shared[end_words(kMaxRanks, 32)];
+  cg::this_cluster().sync();   // every CTA has started, so the first one's shared memory is there; over before the forward's kernel is
   wait_for_stream();
   route_end(a, PartialSums{a.partial, a.experts}, shared);
 }

@@ -49,6 +49,40 @@ def test_formula(comm, dtype, off, counts):
     assert norm(comm, xs, dtype) == norm(comm, xs, dtype)
 
 
+# A tile is 16 KiB of one vector: 32 of them are summed in one launch, 33 in two; the empty vectors between fill no place of the tables of 64 and 1024.
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("tiles", [1, 31, 32, 33])
+def test_one_launch_and_two(comm, dtype, tiles):
+    n = 16384 // torch.finfo(DT[dtype]).bits * 8
+    x = torch.randn(tiles * n, generator=torch.Generator(device="cuda").manual_seed(tiles), device="cuda").to(DT[dtype])
+    empty = x[:0]
+    for xs in ([x], [x[i * n:(i + 1) * n] for i in range(tiles)], [v for i in range(tiles) for v in (empty, empty, empty, x[i * n:(i + 1) * n])] + [empty] * 1100):
+        first = norm(comm, xs, dtype, 5.0)
+        check(first, xs, 5.0)
+        assert norm(comm, xs, dtype, 5.0) == first
+
+
+@pytest.mark.parametrize("k", [64, 65, 1024, 1025, 2049])
+def test_full_tables_with_empty_vectors(comm, k):
+    x = torch.randn(k, 5, generator=torch.Generator(device="cuda").manual_seed(k), device="cuda")
+    xs = [v for row in x for v in (row, row[:0])]
+    check(norm(comm, xs, "fp32"), xs, 1.0)
+
+
+def test_few_tiles_captured(comm):
+    x = torch.randn(9, 4097, device="cuda")
+    t, out = hb.Tensors(list(x), "fp32"), torch.zeros(2, device="cuda")
+    comm.grad_norm(t, out, max_norm=3.0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        comm.grad_norm(t, out, max_norm=3.0, stream=torch.cuda.current_stream())
+    for k in range(3):
+        x.mul_(1.5)
+        graph.replay()
+        check(out.cpu().tolist(), [x.cpu()], 3.0)
+
+
 def test_no_vectors(comm):
     assert norm(comm, [], "fp32") == (0.0, 1.0)
     assert norm(comm, [torch.zeros(5, device="cuda")], "fp32") == (0.0, 1.0)
