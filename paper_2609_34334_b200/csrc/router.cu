@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_kerne
     int here = 0;
 #pragma unroll
     for (int i = 0; i < V; i++) here += x[i] >= bar;
-    if (here) {   // their order does not matter
+    if (here) {   // in places that no order of the lanes is promised for: what follows goes by value and expert alone
       int to = slot * (L * V) + atomicAdd(&candidates[slot], here);
 #pragma unroll
       for (int i = 0; i < V; i++)
@@ -375,20 +375,9 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_kerne
       const unsigned ranked = __ballot_sync(0xffffffffu, rank >= 0) >> (L == 32 ? 0 : group * L) & kLanes;
       const unsigned last = __ballot_sync(0xffffffffu, rank == have - 1 && have) >> (L == 32 ? 0 : group * L) & kLanes;
       done = __all_sync(0xffffffffu, __popc(ranked) == have && (last || !have));
-      if (done) {
-        const float ex = exp_fast(y - top);
-        // 0 * inv: a NaN in the row reaches its weights either way
-        const float part = a.normalize ? lanes_sum<L>(rank >= 0 ? ex : 0.0f) : 1.0f;
-        const float scale = a.normalize ? __fdividef(1.0f, part) + 0.0f * inv : inv;
-        if (rank >= 0) {
-          a.indices[r][at + rank] = (int)own.y;
-          a.weights[r][at + rank] = ex * scale;
-          atomicAdd(&count[own.y], 1);
-        }
-        if (real && lane >= have && lane < a.topk) {
-          a.indices[r][at + lane] = -1;
-          a.weights[r][at + lane] = 0.0f;
-        }
+      if (done && rank >= 0) {
+        chosen[slot][rank] = own;
+        atomicAdd(&count[own.y], 1);
       }
     }
     if (!done) {
@@ -405,14 +394,16 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_kerne
           atomicAdd(&count[own.y], 1);
         }
       }
-      __syncwarp();
-      const uint2 own = lane < have ? chosen[slot][lane] : make_uint2(0, 0xffffffffu);
-      const float ex = lane < have ? exp_fast(__uint_as_float(own.x) - top) : 0.0f;
-      const float part = a.normalize ? lanes_sum<L>(ex) : 1.0f;
-      if (real && lane < a.topk) {
-        a.indices[r][at + lane] = (int)own.y;
-        a.weights[r][at + lane] = lane < have ? ex * (a.normalize ? __fdividef(1.0f, part) + 0.0f * inv : inv) : 0.0f;
-      }
+    }
+    __syncwarp();
+    // the chosen are added in the order of their ranks: the candidates' places, and so the lanes that ranked them, are in no certain order
+    const uint2 own = lane < have ? chosen[slot][lane] : make_uint2(0, 0xffffffffu);
+    const float ex = lane < have ? exp_fast(__uint_as_float(own.x) - top) : 0.0f;
+    const float part = a.normalize ? lanes_sum<L>(ex) : 1.0f;
+    if (real && lane < a.topk) {
+      a.indices[r][at + lane] = (int)own.y;
+      // 0 * inv: a NaN in the row reaches its weights either way
+      a.weights[r][at + lane] = lane < have ? ex * (a.normalize ? __fdividef(1.0f, part) + 0.0f * inv : inv) : 0.0f;
     }
     if (lane == 0) {
       candidates[slot] = 0;

@@ -336,3 +336,33 @@ def test_rows_far_apart():
     before = [x.clone()]
     backward(c, dw, None, [x], dld=ld)
     check_backward(c, dw, None, [x], before)
+
+
+# ------------------------------------------------------------------------------------------------ what a row's neighbours must not change
+
+
+def distinct_rows(T, E, seed=0):
+    """Rows without equal logits."""
+    x = torch.randn(T, E, generator=torch.Generator().manual_seed(seed)).cuda()
+    assert all(r.unique().numel() == E for r in x[:50])
+    return x
+
+
+@pytest.mark.parametrize("E,K", [(32, 4), (61, 4), (64, 8), (128, 8)])
+def test_weights_do_not_depend_on_neighbours_or_the_grid(E, K):
+    """The normalised weights of a row have the same bits beside rows with equal logits, in another place, and in a call of few rows, which lays a row over
+    other lanes: the chosen are added in the order of their ranks."""
+    T = 5000   # beyond the lines to one cluster and to many rows: several rows share a warp
+    x = distinct_rows(T, E)
+    want = Call(1, [T], E, K, "fp32", True, False, [x]).forward()
+    w, i = want.weights[0][:T], want.indices[0][:T]
+    tied = x.clone()
+    tied[1::2] = 1.0
+    got = Call(1, [T], E, K, "fp32", True, False, [tied]).forward()
+    assert torch.equal(got.weights[0][:T:2], w[::2]) and torch.equal(got.indices[0][:T:2], i[::2])
+    order = torch.randperm(T, generator=torch.Generator().manual_seed(1)).cuda()
+    got = Call(1, [T], E, K, "fp32", True, False, [x[order].contiguous()]).forward()
+    assert torch.equal(got.weights[0][:T], w[order]) and torch.equal(got.indices[0][:T], i[order])
+    for at in (0, 16, 2000):
+        got = Call(1, [16], E, K, "fp32", True, False, [x[at:at + 16]]).forward()
+        assert torch.equal(got.weights[0][:16], w[at:at + 16]) and torch.equal(got.indices[0][:16], i[at:at + 16])
