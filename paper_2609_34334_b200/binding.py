@@ -188,11 +188,17 @@ def _state(s) -> int:
 
 
 def _count_of(x, k: int, counts) -> int:
-    if counts is not None:
-        return int(counts[k])
-    if not x.is_contiguous():
-        raise ValueError("tensor %d is not contiguous" % k)
-    return int(x.numel())
+    return int(counts[k]) if counts is not None else int(x.numel())
+
+
+def _check_elements(x, what: str, count: int, size: int) -> None:
+    """A tensor that the library is to take for `count` elements of `size` bytes; an address cannot be checked."""
+    if hasattr(x, "element_size") and (not x.is_contiguous() or x.numel() < count or x.element_size() != size):
+        raise ValueError("%s: %d contiguous elements of %d bytes are wanted" % (what, count, size))
+
+
+# bytes of an element, by the library's numbers for dtypes and states; of numbers that it does not know none is checked: it refuses them
+_DTYPE_SIZE, _STATE_SIZE = {FLOAT32: 4, BFLOAT16: 2}, {0: 4, 1: 1}
 
 
 class Tensors:
@@ -202,6 +208,9 @@ class Tensors:
         self.n, self.dtype, self._keep = len(xs), _dtype(dtype), list(xs)
         self._ptrs = _ptr_array(xs)
         self._counts = (ctypes.c_size_t * self.n)(*[_count_of(x, k, counts) for k, x in enumerate(xs)])
+        if self.dtype in _DTYPE_SIZE:
+            for k, x in enumerate(xs):
+                _check_elements(x, "tensor %d" % k, self._counts[k], _DTYPE_SIZE[self.dtype])
         self._at = ctypes.addressof(self._ptrs), ctypes.addressof(self._counts)
 
 
@@ -221,18 +230,19 @@ class AdamTensors:
             table[k].count = _count_of(params[k], k, counts)
             table[k].weight_decay = float(weight_decay[k]) if hasattr(weight_decay, "__getitem__") else float(weight_decay)
         blocks = [(table[k].count + STATE_BLOCK - 1) // STATE_BLOCK for k in range(n)]
+        param_dtype, grad_dtype, state = _dtype(param_dtype), _dtype(grad_dtype), _state(state)
+        known = param_dtype in _DTYPE_SIZE and grad_dtype in _DTYPE_SIZE and state in _STATE_SIZE
+        size = {"param": _DTYPE_SIZE.get(param_dtype), "grad": _DTYPE_SIZE.get(grad_dtype), "exp_avg": _STATE_SIZE.get(state), "exp_avg_sq": _STATE_SIZE.get(state)}
         for name, xs in lists.items():
             if xs is None:
                 continue
             if len(xs) != n:
                 raise ValueError("%d %s tensors, %d wanted" % (len(xs), name, n))
             for k, x in enumerate(xs):
-                if hasattr(x, "is_contiguous"):
-                    want = blocks[k] if name.endswith("_scale") else table[k].count
-                    if not x.is_contiguous() or x.numel() < want:
-                        raise ValueError("%s[%d]: %d contiguous elements are wanted" % (name, k, want))
+                if known and (state == STATES["8bit"] or not name.endswith("_scale")):   # (scales beside binary32 states are not read)
+                    _check_elements(x, "%s[%d]" % (name, k), blocks[k] if name.endswith("_scale") else table[k].count, size.get(name, 4))
                 setattr(table[k], name, _ptr(x))
-        rc = lib().hoccl_adamw_create(ctypes.byref(self._h), table, n, _dtype(param_dtype), _dtype(grad_dtype), _state(state))
+        rc = lib().hoccl_adamw_create(ctypes.byref(self._h), table, n, param_dtype, grad_dtype, state)
         if rc != OK:
             raise HocclError(rc, "hoccl_adamw_create")
         self._keep = {name: list(xs) for name, xs in lists.items() if xs is not None}

@@ -178,3 +178,34 @@ def test_rates_record():
     import struct
     r = hb.adamw_rates(0.25, 3, 0.5, 0.0, seed=1 << 31 | 5)
     assert struct.unpack("<fffI", bytes(r.numpy().tobytes())) == (0.25, 0.875, 1.0, 1 << 31 | 5)
+
+
+def test_tables_check_the_size_of_elements():
+    """A tensor of the right length whose elements are smaller than the call takes them for would be read, and written, beyond its end."""
+    import torch
+    t = {"fp32": torch.float32, "bf16": torch.bfloat16, "8bit": torch.float8_e4m3fn}
+    good = dict(param="bf16", grad="bf16", m="fp32", v="fp32", master="fp32", ms="fp32", vs="fp32")
+
+    def table(state="fp32", n=256, **kinds):
+        k = {**good, **kinds}
+        x = {name: [torch.zeros(n if name not in ("ms", "vs") else -(-n // 256), dtype=t[kind])] for name, kind in k.items()}
+        return hb.AdamTensors(x["param"], x["grad"], x["m"], x["v"], "bf16", "bf16", state=state, master=x["master"], exp_avg_scale=x["ms"], exp_avg_sq_scale=x["vs"])
+
+    table()
+    table(state="8bit", m="8bit", v="8bit")
+    for bad in (dict(param="fp32"), dict(param="8bit"), dict(grad="fp32"), dict(grad="8bit"), dict(m="bf16"), dict(v="bf16"), dict(master="bf16"), dict(m="8bit")):
+        with pytest.raises(ValueError):
+            table(**bad)
+    for bad in (dict(m="fp32", v="8bit"), dict(m="8bit", v="bf16"), dict(m="8bit", v="8bit", ms="bf16"), dict(m="8bit", v="8bit", vs="bf16")):
+        with pytest.raises(ValueError):
+            table(state="8bit", **bad)
+    with pytest.raises(ValueError):
+        hb.Tensors([torch.zeros(8, dtype=torch.bfloat16)], "fp32")
+    with pytest.raises(ValueError):
+        hb.Tensors([torch.zeros(8)], "bf16")
+    with pytest.raises(ValueError):
+        hb.Tensors([torch.zeros(8)], "fp32", counts=[9])
+    with pytest.raises(ValueError):
+        hb.Tensors([torch.zeros(8)[::2]], "fp32", counts=[4])
+    hb.Tensors([torch.zeros(8)], "fp32", counts=[7])
+    hb.Tensors([torch.zeros(8, dtype=torch.int32)], "fp32")   # four bytes are four bytes
