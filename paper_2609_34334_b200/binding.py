@@ -371,6 +371,10 @@ class Comm:
         self._check(_calls.host_allreduce(self._h.value, h_send, h_recv, count, dtype, op, stream), "hoccl_host_allreduce")
 
     # -- operators of a training step
+    def _check_tokens(self, tokens):
+        if len(tokens) != self.R:   # the library sees R of them: a missing one would be a rank without tokens
+            raise ValueError("%d numbers of tokens, %d wanted" % (len(tokens), self.R))
+
     def adamw(self, tensors: AdamTensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, factor=None, rates=None, seed=0, stream=None):
         """hoccl_adamw_step.  factor: device float (grad_norm's out[1:]); rates: device record (adamw_rates) in place of lr, step and seed."""
         self._check(_calls.adamw_step(self._h.value, tensors._h.value, lr, step, beta1, beta2, eps, grad_scale, factor, rates, seed, stream), "hoccl_adamw_step")
@@ -387,11 +391,13 @@ class Comm:
     def route(self, logits, tokens, experts, topk, dtype, indices, weights, counts, loss, saved, balance_coef=0.01, z_coef=0.0, normalize=True, per_rank=False,
               ld=None, stream=None):
         """ld: elements from one row of the logits to the next (None: experts)."""
+        self._check_tokens(tokens)
         self._check(_calls.route(self._h.value, logits, experts if ld is None else ld, tokens, experts, topk, dtype, normalize, per_rank, balance_coef, z_coef, indices,
                                  weights, counts, loss, saved, stream), "hoccl_route")
 
     def route_backward(self, logits, tokens, experts, topk, dtype, indices, saved, dweights, dloss, dlogits, normalize=True, per_rank=False, ld=None, dld=None,
                        stream=None):
+        self._check_tokens(tokens)
         self._check(_calls.route_backward(self._h.value, logits, experts if ld is None else ld, tokens, experts, topk, dtype, normalize, per_rank, indices, saved, dweights,
                                           dloss, dlogits, experts if dld is None else dld, stream), "hoccl_route_backward")
 

@@ -209,3 +209,16 @@ def test_tables_check_the_size_of_elements():
         hb.Tensors([torch.zeros(8)[::2]], "fp32", counts=[4])
     hb.Tensors([torch.zeros(8)], "fp32", counts=[7])
     hb.Tensors([torch.zeros(8, dtype=torch.int32)], "fp32")   # four bytes are four bytes
+
+
+def test_route_wants_a_number_of_tokens_for_every_rank():
+    c = HostComm(2)
+    c.set_scratch(256 * K, hb.route_scratch_bytes(2, 4, 16))
+    a = dict(logits=[K, 2 * K], experts=16, topk=2, dtype="fp32", indices=[3 * K, 4 * K], weights=[5 * K, 6 * K], counts=[7 * K, 8 * K], loss=9 * K, saved=10 * K, stream=0)
+    b = dict(logits=[K, 2 * K], experts=16, topk=2, dtype="fp32", indices=[3 * K, 4 * K], saved=10 * K, dweights=[5 * K, 6 * K], dloss=None, dlogits=[11 * K, 12 * K], stream=0)
+    for tokens in ([4], [], [4, 3, 2]):
+        with pytest.raises(ValueError):
+            c.route(tokens=tokens, **a)
+        with pytest.raises(ValueError):
+            c.route_backward(tokens=tokens, **b)
+    assert code(c.route, tokens=[4, 3], **a) == hb.ERR_CUDA and code(c.route_backward, tokens=(4, 3), **b) == hb.ERR_CUDA
