@@ -540,7 +540,7 @@ typedef struct {
 } hoccl_adamw_rates_t;
 
 typedef struct {
-  double lr, beta1, beta2, eps;  /* finite, in binary32 too; 0 <= beta < 1; eps a positive normal binary32 number */
+  double lr, beta1, beta2, eps;  /* finite, in binary32 too; 0 <= beta < 1; 2^-126 <= eps <= 2^126 */
   double grad_scale;             /* the gradients are multiplied by it (1 / R for a mean over R ranks) */
   long step;                     /* 1 for the first */
   uint32_t seed;                 /* HOCCL_STATE_8BIT: of the rounding; another one each step */

@@ -755,7 +755,7 @@ bool fill_scalars(const hoccl_adamw_config_t& c, AdamScalars* s) {
   s->rates = c.rates;
   for (float x : {s->lr, s->step_size, s->root_scale, s->grad_scale})
     if (!std::isfinite(x)) return false;
-  return eps >= 1.17549435e-38f;   // the kernels divide by numbers from eps on with a reciprocal that takes normal ones
+  return eps >= 0x1p-126f && eps <= 0x1p126f;   // the kernels divide by numbers from eps on with a reciprocal that takes and gives normal ones, else 0
 }
 
 struct Region {

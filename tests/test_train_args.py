@@ -222,3 +222,10 @@ def test_route_wants_a_number_of_tokens_for_every_rank():
         with pytest.raises(ValueError):
             c.route_backward(tokens=tokens, **b)
     assert code(c.route, tokens=[4, 3], **a) == hb.ERR_CUDA and code(c.route_backward, tokens=(4, 3), **b) == hb.ERR_CUDA
+
+
+def test_an_eps_whose_reciprocal_is_not_normal_is_refused():
+    """The step divides by numbers from eps on with a reciprocal that gives 0 where the true one is below the least normal number."""
+    c, t = HostComm(2), plan([row()])
+    for eps, want in ((2.0 ** 126, hb.ERR_CUDA), (1e38, hb.ERR_INVALID_ARG), (3e38, hb.ERR_INVALID_ARG)):
+        assert code(c.adamw, t, lr=1e-3, step=1, eps=eps, stream=0) == want
