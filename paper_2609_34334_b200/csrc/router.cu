@@ -64,6 +64,16 @@ __device__ __forceinline__ float lanes_max(float x) {
   }
 }
 template <int L>
+__device__ __forceinline__ unsigned lanes_min(unsigned x) {
+  if constexpr (L == 32) {
+    return __reduce_min_sync(0xffffffffu, x);
+  } else {
+#pragma unroll
+    for (int d = L / 2; d; d >>= 1) x = min(x, __shfl_xor_sync(0xffffffffu, x, d));
+    return x;
+  }
+}
+template <int L>
 __device__ __forceinline__ float lanes_sum(float x) {
 #pragma unroll
   for (int d = L / 2; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
@@ -293,7 +303,11 @@ __global__ void __launch_bounds__(1024) route_end_kernel(const __grid_constant__
 
 // The topk largest of a row without a pass over it for each: the topk-th largest of the lanes' own largest logits is a bar that at least topk logits reach, and
 // few more do (a dozen for 8 of 256); those are collected.  Where a lane can hold each of them and no two are alike, a maximum over the warp finds one after
-// the other; else each counts the ones in front of it.  (One search of the whole row for each choice took 1090 instructions a row of 256 and 50 us for
+// the other; up to twice as many, or with some alike, each counts the ones in front of it.  More of them (rows of many equal logits, the bar of which few are
+// below; up to all experts) are searched topk times, each lane its share: counting would take the square of their number.
+// us for 8 ranks of n rows with counting up to 1, 2 and 4 times the lanes, and whatever the number: 128 experts, topk 8, n = 2048 18.8, 16.7, 16.7, 16.7;
+// 256 experts, topk 32, n = 4096 130, 129, 144, 168; 256 experts, topk 8, n = 4096 26.6 each, all logits alike 74, 74, 74, 629.
+// (One search of the whole row for each choice took 1090 instructions a row of 256 and 50 us for
 // 32,000 rows, most of it on the half-rate integer pipe; this form takes 23 us, 6 of them for ranking and writing, 5.3 for the bar and the collecting.)
 template <int DT, int V, int L, bool VEC>
 __global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_kernel(const __grid_constant__ RouteArgs a) {
@@ -380,7 +394,7 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_kerne
         atomicAdd(&count[own.y], 1);
       }
     }
-    if (!done) {
+    if (!done && (V <= 2 || __all_sync(0xffffffffu, n <= 2 * L))) {
       for (int c = lane; c < n; c += L) {
         const uint2 own = mine[c];
         const float y = __uint_as_float(own.x);
@@ -392,6 +406,34 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_kerne
         if (before < a.topk) {
           chosen[slot][before] = own;
           atomicAdd(&count[own.y], 1);
+        }
+      }
+    } else if (V > 2 && !done) {
+      // a lane offers the first of its share of what is left
+      float best;
+      unsigned first, from;
+      const auto offer = [&] {
+        best = -INFINITY;
+        first = ~0u;
+        for (unsigned c = lane; c < (unsigned)n; c += L) {
+          const uint2 o = mine[c];
+          const float y = __uint_as_float(o.x);
+          if (y > best || (y == best && o.y < first)) {
+            best = y;
+            first = o.y;
+            from = c;
+          }
+        }
+      };
+      offer();
+      for (int k = 0; k < a.topk; k++) {
+        const float v = lanes_max<L>(best);
+        const unsigned e = lanes_min<L>(best == v ? first : ~0u);
+        if (first == e && e != ~0u) {   // one lane, as an expert has one place; none where nothing is left
+          chosen[slot][k] = make_uint2(__float_as_uint(best), e);
+          atomicAdd(&count[e], 1);
+          mine[from].x = 0x7fc00000u;
+          offer();
         }
       }
     }

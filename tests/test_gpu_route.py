@@ -366,3 +366,44 @@ def test_weights_do_not_depend_on_neighbours_or_the_grid(E, K):
     for at in (0, 16, 2000):
         got = Call(1, [16], E, K, "fp32", True, False, [x[at:at + 16]]).forward()
         assert torch.equal(got.weights[0][:16], w[at:at + 16]) and torch.equal(got.indices[0][:16], i[at:at + 16])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("E,K", [(32, 4), (64, 8), (61, 6), (128, 12), (256, 8), (512, 32), (1024, 32)])
+def test_rows_of_many_equal_logits(E, K, dtype):
+    """All alike; alike but for a few above, below or closed; two or three values; next to rows without equal ones; in one cluster and in many CTAs."""
+    for T in (24, 4500 if E <= 256 else 600):
+        g = torch.Generator().manual_seed(E + T)
+        x = torch.randn(T, E, generator=g)
+        x[0::6] = 0.0
+        x[1::6] = torch.randint(0, 2, (len(x[1::6]), E), generator=g).float() * 0.5
+        x[2::6] = torch.randint(-1, 2, (len(x[2::6]), E), generator=g).float()
+        few = torch.rand(len(x[3::6]), E, generator=g)
+        x[3::6] = torch.where(few < 0.02, few * 50, torch.where(few > 0.98, -1.0, -0.0))
+        x[4::6] = torch.where(torch.rand(len(x[4::6]), E, generator=g) < 0.7, -math.inf, 2.0)
+        c = Call(1, [T], E, K, dtype, True, False, [x.cuda().to(DT[dtype])])
+        c.forward().check()
+
+
+def per_call_us(c, reps=5):
+    for _ in range(2):
+        c.forward()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    e0.record()
+    for _ in range(reps):
+        c.forward()
+    e1.record()
+    torch.cuda.synchronize()
+    return e0.elapsed_time(e1) * 1e3 / reps
+
+
+@pytest.mark.parametrize("E,K,times", [(64, 4, 6), (256, 8, 6), (1024, 32, 8)])
+def test_equal_logits_are_not_far_slower(E, K, times):
+    """A router that starts from zeros, rows of padding that are not masked: such a row's choice takes topk searches of what a lane holds (E / 32 logits or
+    so) and a maximum over the lanes, where another row's takes two maxima: a small multiple, not a number that grows with the square of the experts."""
+    T = 32_000
+    x = torch.randn(T, E, device="cuda")
+    usual = per_call_us(Call(1, [T], E, K, "fp32", True, False, [x]))
+    alike = per_call_us(Call(1, [T], E, K, "fp32", True, False, [torch.zeros_like(x)]))
+    print("%d experts, topk %d: %.1f us, all alike %.1f us" % (E, K, usual, alike))
+    assert alike < times * usual
