@@ -611,12 +611,13 @@ hoccl_result_t hoccl_grad_norm(const void* const* grads, const size_t* counts, i
  * (`per_rank`: R groups), with f_e = count of e / (topk * n) and P_e = the rows' sum of p_e / n:
  *   loss[0] = balance_coef * experts * sum of f_e P_e;  loss[1] = z_coef * (the rows' sum of log(sum of exp(logits))^2) / n; both 0 if n is 0;
  *   saved = balance_coef * experts * f_e / n for each expert, then 2 * z_coef / n: what hoccl_route_backward needs.
- * A NaN logit is never chosen; it makes its row's weights and the losses NaN, as +infinity does.  The dtype's lowest number is a logit like any other: such a row is no
- * padding, and its logarithm's square is infinite (loss[1] is 0 all the same if z_coef is 0).  counts are exact, f and P summed in a fixed order.
+ * A NaN logit is never chosen; it makes its row's weights and both losses NaN, as +infinity does.  A row with a NaN and nothing else
+ * above -infinity chooses nothing and counts nowhere, but the losses are NaN.  The dtype's lowest number is a logit like any other: such a row is no
+ * padding, and its logarithm's square is infinite.  loss[1] is 0 whatever the logits are if z_coef is 0.  counts are exact, f and P summed in a fixed order.
  *
  * hoccl_route_backward: dlogits[r] (rows of `dld` elements) = dloss[group] * d(loss[0] + loss[1])/dlogits, f held fixed, + the gradient that dweights[r] (tokens[r] x topk)
  * gives through the weights; with `logits`, `indices`, `saved`, the shape and the flags of the forward call.  dloss: DEVICE floats, one for each group, NULL for ones;
- * dweights: NULL for none.  Entries of dweights beside an index outside 0 .. experts-1 are ignored; rows without an open expert get zeros.
+ * dweights: NULL for none.  Entries of dweights beside an index outside 0 .. experts-1 are ignored; rows whose logits are all -infinity get zeros, rows with a NaN get NaN.
  * dlogits[r] may be logits[r] with dld == ld; what lies between the rows is left as it is.
  *
  * indices, weights, dweights, counts: contiguous.  1 <= topk <= min(32, experts), experts <= 1024, tokens[r] < 2^31 (0: that rank's pointers may be NULL, but counts[r] is written).

@@ -130,7 +130,7 @@ __device__ __forceinline__ void load_row(const void* base, unsigned long long at
 }
 
 // Row whose largest logit is `top`: x -> exp(x - top); their sum and its reciprocal.  A row without a logit above -infinity:
-// 0, NaN where the logit is, inv 1, and false (top is set to 0).
+// 0, NaN where the logit is; their sum 0 or NaN, inv 1, and false (top is set to 0).
 template <int V, int L>
 __device__ __forceinline__ bool softmax_row(float* x, float* top, float* total, float* inv) {
   const bool open = *top > -INFINITY;
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(kWarpsFor<V> * 32, V <= 8 ? 2 : 1) route_kerne
     for (int i = 0; i < V; i++) p_sum[i] += x[i] * inv;
     if (lane == turn) {                  // a logarithm takes as long for one lane as for all: each lane keeps a row's until all have one
       log_top = top;
-      log_total = open ? total : 1.0f;
+      log_total = open ? total : total + 1.0f;   // closed: 1, or NaN
     }
     if (++turn == L) {
       const float s = log_top + logf(log_total);

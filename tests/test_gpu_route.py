@@ -407,3 +407,25 @@ def test_equal_logits_are_not_far_slower(E, K, times):
     alike = per_call_us(Call(1, [T], E, K, "fp32", True, False, [torch.zeros_like(x)]))
     print("%d experts, topk %d: %.1f us, all alike %.1f us" % (E, K, usual, alike))
     assert alike < times * usual
+
+
+@pytest.mark.parametrize("T", [4, 5000])
+@pytest.mark.parametrize("E", [8, 61, 256])
+@pytest.mark.parametrize("row", ["one", "all", "rest closed"])
+def test_a_nan_reaches_both_losses(row, E, T):
+    """One row of a call alone: a NaN among numbers, nothing but NaN, NaN with the rest closed (the last two choose nothing and count nowhere)."""
+    x = torch.randn(T, E, device="cuda")
+    if row == "rest closed":
+        x[1] = -math.inf
+    x[1, 3 if row != "all" else slice(None)] = math.nan
+    c = Call(1, [T], E, 3, "fp32", True, False, [x]).forward()
+    assert c.loss[0].isnan() and c.loss[1].isnan()
+    assert int(c.counts[0, E]) == (T if row == "one" else T - 1)
+    assert c.saved[:E + 1].isfinite().all()
+    out = [torch.zeros(T, E, device="cuda")]
+    backward(c, [torch.ones(T, 3, device="cuda")], None, out)
+    assert out[0][1].isnan().all() and out[0][0].isfinite().all() and out[0][2:].isfinite().all()
+    c = Call(1, [1], E, 3, "fp32", True, False, [x[1:2]]).forward()   # and as the only row
+    assert c.loss[0].isnan() and c.loss[1].isnan() and c.saved[:E + 1].isfinite().all()
+    c.comm.route(c.x, c.tokens, E, 3, "fp32", c.indices, c.weights, list(c.counts), c.loss, c.saved, balance_coef=BAL, z_coef=0.0)
+    assert c.loss[0].isnan() and float(c.loss[1]) == 0.0
