@@ -582,7 +582,7 @@ hoccl_result_t hoccl_adamw_step(hoccl_adamw_plan_t plan, const hoccl_adamw_confi
  * first element on (blocks of 8-bit states too; c is the tensor's number h).  The gradient of chunk c is grad_scale * factor * (((x_{c+1} + x_{c+2}) + ...) + x_c):
  * the ring's order of adds, in binary32 and, unlike hoccl_reduce_scatter, never rounded to the gradients' dtype in between.  The new weights go to every
  * params[r]; without masters they are computed from params[c].  The step with a clipped norm, which needs the summed gradient first, is hoccl_reduce_scatter,
- * hoccl_grad_norm, hoccl_adamw_step on the shards, hoccl_allgather.  No scratch.
+ * hoccl_grad_norm, hoccl_adamw_step on the shards, hoccl_allgather (hoccl_grad_norm says what max_norm a mean takes).  No scratch.
  * master: NULL or R pointers; the scales may be NULL with HOCCL_STATE_FLOAT32.  Pointers of an empty chunk may be NULL.  No two arrays may overlap.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA as hoccl_adamw_create and hoccl_adamw_step.
  */
@@ -594,7 +594,9 @@ hoccl_result_t hoccl_sharded_adamw(const void* const* grads, void* const* params
 /*
  * Norm of the n vectors grads[k] (counts[k] elements each) as one vector: out[0] = sqrt(sum of squares), summed in binary64, and
  * out[1] = min(1, max_norm / (out[0] + 1e-6)), the factor that clips to max_norm; NaN if a gradient is not finite.  out: two DEVICE floats.
- * max_norm > 0, infinity for no clipping.  Needs hoccl_grad_norm_scratch_bytes() of scratch.  Empty vectors may be NULL; no vectors: 0 and 1.
+ * max_norm > 0, infinity for no clipping.  Both are of the gradients as they lie in memory: hoccl_adamw_step's grad_scale multiplies what the factor has clipped.  With sums
+ * over R ranks and grad_scale = 1 / R, max_norm = R * m clips the mean to m, and the mean's norm is out[0] / R.
+ * Needs hoccl_grad_norm_scratch_bytes() of scratch.  Empty vectors may be NULL; no vectors: 0 and 1.
  * Errors: INVALID_ARG (NULL, misaligned, max_norm), UNSUPPORTED (dtype), SCRATCH, CUDA.
  */
 size_t hoccl_grad_norm_scratch_bytes(void);

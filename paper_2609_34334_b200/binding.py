@@ -385,7 +385,8 @@ class Comm:
                                          _state(state), weight_decay, lr, step, beta1, beta2, eps, grad_scale, factor, rates, seed, stream), "hoccl_sharded_adamw")
 
     def grad_norm(self, grads: Tensors, out, max_norm=float("inf"), stream=None):
-        """out: two device floats, the norm and the factor that clips to max_norm."""
+        """out: two device floats, the norm and the factor that clips to max_norm, both of the gradients as they lie in memory (sums over R ranks that adamw scales
+        by 1 / R: max_norm = R * the mean's)."""
         self._check(_calls.grad_norm(self._h.value, grads._at[0], grads._at[1], grads.n, grads.dtype, max_norm, out, stream), "hoccl_grad_norm")
 
     def route(self, logits, tokens, experts, topk, dtype, indices, weights, counts, loss, saved, balance_coef=0.01, z_coef=0.0, normalize=True, per_rank=False,

@@ -417,7 +417,7 @@ def step(args):
         def clipped(k):
             j = k % pool
             comm.reduce_scatter(grads[j], shards[j], q, "bf16", stream)
-            comm.grad_norm(lists[j], norm, max_norm=1.0, stream=stream)
+            comm.grad_norm(lists[j], norm, max_norm=1.0 * R, stream=stream)   # of the sums: their mean is clipped to 1
             comm.adamw(tables[j], 1e-4, k + 1, grad_scale=1.0 / R, factor=norm[1:], seed=k, stream=stream)
             comm.allgather(own, params, q, "bf16", stream)
 

@@ -212,3 +212,50 @@ def test_the_current_device_and_stream_stay():
         assert torch.cuda.current_stream() == side and torch.cuda.current_device() == 0
     torch.cuda.synchronize()
     comm.destroy()
+
+
+@pytest.mark.parametrize("R,limit", [(4, 0.5), (8, 3.0), (3, 1e3)])
+def test_the_clipped_step_of_a_mean(R, limit):
+    """Gradients that are a mean over the ranks (grad_scale 1 / R): the norm is that of the sums as they lie in memory, so clipping the mean to `limit` takes a max_norm of
+    limit * R."""
+    q = 3000
+    comm = communicator(R, R * q)
+    s = Shards(R, q, "fp32", seed=R)
+    table, sums = s.table(), hb.Tensors(s.sums, "fp32")
+    comm.reduce_scatter(s.grads, s.sums, q, "fp32")
+    comm.grad_norm(sums, s.norm, max_norm=limit * R)
+    comm.adamw(table, 1e-2, 1, grad_scale=1.0 / R, factor=s.norm[1:])
+    torch.cuda.synchronize()
+    mean = sum(g.double() for g in s.grads) / R
+    n = float(mean.norm())
+    clipped = mean * min(1.0, limit / n)
+    # (1 - beta1) * clipped: up to 8 adds of the sum, the factor's own rounding and 6 more of binary32; 1e-6 / (R n) of the factor's guard
+    tol = (16 * 2.0 ** -24 + 1e-6 / (R * n)) * 0.1 * min(1.0, limit / n) * sum(g.double().abs() for g in s.grads) / R
+    assert ((torch.cat(s.m).double() - 0.1 * clipped).abs() <= tol).all()
+    assert (n > limit) == (limit < 1e3)
+    comm.destroy()
+
+
+def test_the_sweep_clips_the_mean(monkeypatch, capsys):
+    """The step command's clipped form: what it clips to, after the mean's scale, is a norm of 1."""
+    from types import SimpleNamespace
+
+    from paper_2609_34334_b200 import sweep
+
+    clips, scales = [], []
+    norm, adamw = hb.Comm.grad_norm, hb.Comm.adamw
+
+    def seen_norm(self, grads, out, max_norm=float("inf"), stream=None):
+        clips.append(max_norm)
+        return norm(self, grads, out, max_norm=max_norm, stream=stream)
+
+    def seen_adamw(self, tensors, lr, step, **more):
+        scales.append(more["grad_scale"])
+        return adamw(self, tensors, lr, step, **more)
+
+    monkeypatch.setattr(hb.Comm, "grad_norm", seen_norm)
+    monkeypatch.setattr(hb.Comm, "adamw", seen_adamw)
+    sweep.step(SimpleNamespace(buckets=1))
+    assert len(clips) == len(scales) > 0
+    assert all(abs(c * s - 1.0) < 1e-12 for c, s in zip(clips, scales)), (clips[0], scales[0])
+    assert '"delivered_bit_exact": true' in capsys.readouterr().out
