@@ -596,7 +596,7 @@ hoccl_result_t hoccl_sharded_adamw(const void* const* grads, void* const* params
  * out[1] = min(1, max_norm / (out[0] + 1e-6)), the factor that clips to max_norm; NaN if a gradient is not finite.  out: two DEVICE floats.
  * max_norm > 0, infinity for no clipping.  Both are of the gradients as they lie in memory: hoccl_adamw_step's grad_scale multiplies what the factor has clipped.  With sums
  * over R ranks and grad_scale = 1 / R, max_norm = R * m clips the mean to m, and the mean's norm is out[0] / R.
- * Needs hoccl_grad_norm_scratch_bytes() of scratch.  Empty vectors may be NULL; no vectors: 0 and 1.
+ * Needs hoccl_grad_norm_scratch_bytes() of scratch.  Empty vectors may be NULL; no vectors: a norm of 0.
  * Errors: INVALID_ARG (NULL, misaligned, max_norm), UNSUPPORTED (dtype), SCRATCH, CUDA.
  */
 size_t hoccl_grad_norm_scratch_bytes(void);

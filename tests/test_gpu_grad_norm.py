@@ -121,3 +121,9 @@ def test_more_elements_than_32_bits_count(comm):
     x = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
     x[0], x[1 << 31], x[n - 1] = 3.0, 4.0, 12.0
     assert norm(comm, [x], "bf16", 26.0) == (13.0, 1.0)
+
+
+@pytest.mark.parametrize("max_norm", [1.0, 1e-6, 1e-7])
+def test_no_vectors(comm, max_norm):
+    """A norm of 0, and the factor that the formula gives for it."""
+    check(norm(comm, [], "fp32", max_norm), [], max_norm)
