@@ -58,8 +58,8 @@ struct AdamRow {
   float decay;
   unsigned flags;   // bit 0: aligned for eight elements at a time; the rest: number of the tensor in the caller's table
 };
-// Tensors by value: a launch carries up to 32 (2.4 KB of parameters; a call takes 2.9 us of the host's time), 96 (7 KB, 3.2 us) or 420 (32 KB, the most there
-// is, 5.0 us).
+// Tensors by value: a launch carries up to 32 (2.4 KB of parameters; a call takes 2.9 us of the host's time), 128 (9.4 KB, 3.1 us) or 420 (31 KB, about the most
+// there is, 3.9 us).  With 64 in the middle a call of 96 tensors takes 3.9 us, with 96 3.0, with 128 3.1, with 192 3.3; one of 128 tensors 3.9, 3.9, 3.1 and 3.3.
 template <int N>
 struct AdamTableT {
   int n, pad;
@@ -67,7 +67,7 @@ struct AdamTableT {
   unsigned first[N + 1];        // prefix sums of tiles: a CTA each
 };
 using AdamTableSmall = AdamTableT<32>;
-using AdamTableMiddle = AdamTableT<96>;
+using AdamTableMiddle = AdamTableT<128>;
 using AdamTable = AdamTableT<420>;
 static_assert(sizeof(AdamTable) + sizeof(AdamScalars) <= 32764, "kernel parameters");
 
@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(kOptThreads, 32 / kWarps) adamw_kernel(const _
   if (r.skip) return;
   const unsigned tile = blockIdx.x, here = (threadIdx.x & ~31u) * 8;
   int k = 0;
-  for (int step = t.n <= 32 ? 16 : t.n <= 96 ? 64 : 256; step; step >>= 1)   // the tensor the tile lies in
+  for (int step = t.n <= 32 ? 16 : t.n <= 128 ? 64 : 256; step; step >>= 1)   // the tensor the tile lies in
     if (k + step < t.n && t.first[k + step] <= tile) k += step;
   const AdamRow& row = t.row[k];
   const unsigned long long at = (unsigned long long)(tile - t.first[k]) * kTile;

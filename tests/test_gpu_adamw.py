@@ -538,3 +538,9 @@ def test_sharded_adds_in_the_rings_order(grad):
             acc = (acc + g[(c + j) % R][a:b]).astype(np.float32)
         assert np.array_equal(acc, d["m"][c].cpu().numpy()[:b - a])
     comm.destroy()
+
+
+@pytest.mark.parametrize("state", ["fp32", "8bit"])
+@pytest.mark.parametrize("n", [32, 127, 128, 129])
+def test_numbers_of_tensors_at_the_tables_ends(comm, n, state):
+    test_many_tensors(comm, n, state)
