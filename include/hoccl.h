@@ -513,7 +513,7 @@ hoccl_result_t hoccl_allreduce_static(const void* const* send, void* const* recv
  * at the call stays current.  Nothing is allocated, so every call may be captured into a graph.  In handshake mode they are launched into
  * the caller's stream like any other kernel.  They use the whole GPU ("sum_ctas" and "copy_ctas" do not bound them).  A call's results do
  * not depend on what else runs; the same call on the same inputs gives the same bits.
- * Calls with scratch use what hoccl_comm_set_scratch attached: calls that overlap in time on different streams need communicators of their own.
+ * Calls with scratch use what hoccl_comm_set_scratch attached, which no buffer of the call may overlap (INVALID_ARG): calls that overlap in time on different streams need communicators of their own.
  */
 
 /* How the averages of an AdamW step are kept: as binary32 numbers, or as e4m3 numbers (8 bits) with one binary32 scale for each block of

@@ -1032,14 +1032,17 @@ extern "C" hoccl_result_t hoccl_grad_norm(const void* const* grads, const size_t
   if (!e) return HOCCL_ERR_UNSUPPORTED;
   unsigned long long tiles = 0;
   int vectors = 0;
+  const size_t need = hoccl_grad_norm_scratch_bytes();
+  const auto in_scratch = [&](const void* p, size_t bytes) { return c->scratch && ranges_overlap((const char*)c->scratch, need, (const char*)p, bytes); };
+  if (in_scratch(out, 8)) return HOCCL_ERR_INVALID_ARG;
   for (int k = 0; k < n; k++) {
     if (!counts[k]) continue;
-    if (!grads[k] || !aligned_to(grads[k], e) || counts[k] > kMaxTensorElements) return HOCCL_ERR_INVALID_ARG;
+    if (!grads[k] || !aligned_to(grads[k], e) || counts[k] > kMaxTensorElements || in_scratch(grads[k], counts[k] * e)) return HOCCL_ERR_INVALID_ARG;
     tiles += norm_tiles(counts[k], e);
     vectors++;
   }
   if (tiles >= (1ull << 32) - kNormCtas) return HOCCL_ERR_INVALID_ARG;   // (a CTA's tile number passes the last one by a grid)
-  if (!c->scratch || c->scratch_bytes < hoccl_grad_norm_scratch_bytes()) return HOCCL_ERR_SCRATCH;
+  if (!c->scratch || c->scratch_bytes < need) return HOCCL_ERR_SCRATCH;
   c->stats = hoccl_stats_t{};
   DeviceScope scope(c->device);
   CU_TRY(c, scope.err);

@@ -763,6 +763,11 @@ hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* t
   a.per_choice = 1.0 / f->topk;
   a.loss = loss;
   a.saved_out = saved;
+  // the bar of the choice is the topk-th of as many numbers as there are lanes: few of them would let many logits over it
+  const int wide = shape_with(32, f->experts), compact = compact_shape(f->experts, 2 * f->topk);
+  int shape = wide;
+  unsigned grid = share_rows(tokens, c->R, wide, kRouteCtas, &a.rows_per_cta, a.first);
+  const size_t need = (size_t)grid * (2 * (size_t)f->experts + 2) * sizeof(float);
   bool vec = (f->experts * e) % 16 == 0 && (ld * e) % 16 == 0;
   try {
     std::vector<Span> spans = {{(const char*)loss, 8u * (size_t)groups, true}, {(const char*)saved, (size_t)groups * (f->experts + 1) * 4, true}};
@@ -781,15 +786,11 @@ hoccl_result_t hoccl_route(const void* const* logits, size_t ld, const size_t* t
       spans.push_back({(const char*)indices[r], tokens[r] * f->topk * 4, true});
       spans.push_back({(const char*)weights[r], tokens[r] * f->topk * 4, true});
     }
+    if (c->scratch) spans.push_back({(const char*)c->scratch, need, true});
     if (spans_clash(&spans)) return HOCCL_ERR_INVALID_ARG;
   } catch (const std::bad_alloc&) {
     return HOCCL_ERR_INTERNAL;
   }
-  // the bar of the choice is the topk-th of as many numbers as there are lanes: few of them would let many logits over it
-  const int wide = shape_with(32, f->experts), compact = compact_shape(f->experts, 2 * f->topk);
-  int shape = wide;
-  unsigned grid = share_rows(tokens, c->R, wide, kRouteCtas, &a.rows_per_cta, a.first);
-  const size_t need = (size_t)grid * (2 * (size_t)f->experts + 2) * sizeof(float);
   bool one_cluster = grid && share_in_cluster(tokens, c->R, wide, &a.rows_per_cta, a.first);   // ends by itself
   if (grid && !one_cluster && compact != wide) {
     one_cluster = share_in_cluster(tokens, c->R, compact, &a.rows_per_cta, a.first);

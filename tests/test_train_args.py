@@ -229,3 +229,23 @@ def test_an_eps_whose_reciprocal_is_not_normal_is_refused():
     c, t = HostComm(2), plan([row()])
     for eps, want in ((2.0 ** 126, hb.ERR_CUDA), (1e38, hb.ERR_INVALID_ARG), (3e38, hb.ERR_INVALID_ARG)):
         assert code(c.adamw, t, lr=1e-3, step=1, eps=eps, stream=0) == want
+
+
+def test_scratch_that_overlaps_a_callers_buffer_is_refused():
+    c = HostComm(2)
+    need = hb.grad_norm_scratch_bytes()
+    c.set_scratch(8 * K, need + 4096)
+    inside, behind, across = 8 * K + need - 4, 8 * K + need, 8 * K - 16
+    for at, want in ((inside, hb.ERR_INVALID_ARG), (across, hb.ERR_INVALID_ARG), (behind, hb.ERR_CUDA), (8 * K - 32, hb.ERR_CUDA)):
+        assert code(c.grad_norm, hb.Tensors([K, at], "fp32", counts=[5, 8]), 64, stream=0) == want, at
+    for out, want in ((inside - 4, hb.ERR_INVALID_ARG), (8 * K - 4, hb.ERR_INVALID_ARG), (behind, hb.ERR_CUDA), (8 * K - 8, hb.ERR_CUDA)):
+        assert code(c.grad_norm, hb.Tensors([K], "fp32", counts=[5]), out, stream=0) == want, out
+    a = dict(logits=[K, 2 * K], tokens=[4, 3], experts=16, topk=2, dtype="fp32", indices=[3 * K, 4 * K], weights=[5 * K, 6 * K], counts=[7 * K, 9 * K], loss=10 * K, saved=11 * K, stream=0)
+    assert code(c.route, **a) == hb.ERR_CUDA
+    used = 2 * (2 * 16 + 2) * 4   # two ranks with one CTA each
+    assert used <= hb.route_scratch_bytes(2, 4, 16) <= need
+    for at, want in ((8 * K, hb.ERR_INVALID_ARG), (8 * K + used - 4, hb.ERR_INVALID_ARG), (8 * K - 4, hb.ERR_INVALID_ARG), (8 * K + 4096, hb.ERR_CUDA), (8 * K - 1024, hb.ERR_CUDA)):
+        for name in ("logits", "indices", "weights", "counts"):
+            assert code(c.route, **{**a, name: [a[name][0], at]}) == want, (name, at)
+        for name in ("loss", "saved"):
+            assert code(c.route, **{**a, name: at}) == want, (name, at)
