@@ -3,7 +3,8 @@
 //
 // All three stream.  An element of a bf16 weight with a binary32 master and states moves 28 bytes (gradient 2, master, m and v 4 in and 4 out, weight 2 out) and
 // takes 35 instructions: HBM bounds it (201 M weights 821 us, 6.87 TB/s).  With 8-bit states it moves 16 bytes and takes 70: the issue of
-// instructions bounds it (541 to 570 us, 5.7 to 6.0 TB/s), so its arithmetic goes two numbers an instruction and every step of the rounding is counted.
+// instructions bounds it (548 to 573 us with the same arrays again and again, 585 to 591 with three sets in turn: 5.5 TB/s), so its arithmetic goes two numbers an
+// instruction and every step of the rounding is counted.
 // The unit of work is a block of 256 elements, one warp's: the elements that share a scale in 8-bit states, so that a block's
 // largest value is one warp reduction and states of either kind have one shape.  In an aligned, whole block lane l holds elements 8 l .. 8 l + 7 (32-byte
 // accesses of binary32 arrays, 16 of bf16, 8 of codes); in any other one elements l, l + 32, ...  Both run the same arithmetic: alignment changes no bit.
@@ -161,7 +162,9 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either 
 }
 
 // How a block is read and written: element by element within the array's end, element by element all of it, two elements at a time (arrays that start on two
-// elements' boundary; the sharded step alone: half as many accesses of every rank's arrays, where the plain step gains nothing), or eight (on 8 elements').
+// elements' boundary; the sharded step alone: half as many accesses of every rank's arrays), or eight (on 8 elements').  The plain step takes elements one by one
+// wherever it cannot take eight.  Pairs would serve arrays on two elements' boundary alone: 50 M weights there, one by one and in pairs, bf16 with master
+// 213 and 208 us, without 179 and 162, with 8-bit states 166 and 144; arrays one element off 213, 180 and 166.
 enum Mode { ENDS, WHOLE, PAIRS, VECTORS };
 // Where a thread's eight elements lie in its tile, and whether they exist where `left` elements do.
 template <Mode MODE>
@@ -508,7 +511,8 @@ __global__ void __launch_bounds__(kOptThreads, 32 / kWarps) adamw_kernel(const _
 // The gradients of a block are read from every rank at once and its new weights stored to every rank: the reads and writes of an all-reduce, with the state's in
 // between.  13.1 M bf16 weights over 8 ranks: 117 us, 6.3 TB/s (with four of eight gradients in flight and 170 registers 278 us; the pair of collectives alone 211);
 // one weight more, which puts chunks off 32 bytes, 129 us (two elements at a time in every other chunk, one in the rest; 139 with one in all; 146 with 80 registers
-// instead of 64, 175 with 128 and all eight gradients in flight).
+// instead of 64, 175 with 128 and all eight gradients in flight).  64 registers make ten of the twelve forms spill, 8 to 44 bytes: 2 us more for the aligned
+// weights, 7 less for the others, taken one at a time.
 template <int GT, int W, int STATE, Mode MODE>
 __device__ __forceinline__ void sharded_block(const ShardedArgs& args, const AdamScalars& s, const Rates& r, int c, unsigned long long lo, const Place& a) {
   // the ring's order: c + 1, c + 2, ..., c; the gradients of kFlight ranks in flight at a time, as they lie in memory
@@ -584,7 +588,7 @@ using NormTableSmall = NormTableT<64>;
 using NormTable = NormTableT<kNormRows>;
 static_assert(sizeof(NormTable) <= 32764, "kernel parameters");
 
-// 201 M bf16 gradients: 63 us, 6.4 TB/s.  Squares in binary64: the square of any binary32 number is there, and a long sum keeps its bits.
+// 201 M bf16 gradients: 62 to 69 us from one GPU to another, 6.5 to 5.8 TB/s.  Squares in binary64: the square of any binary32 number is there, and a long sum keeps its bits.
 template <int DT>
 __device__ __forceinline__ double squares(uint4 r) {
   float x[8];
